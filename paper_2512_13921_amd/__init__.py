@@ -33,7 +33,9 @@ __all__ = ["SwrError", "swr_forward", "swr_backward", "swr_carriers", "swr_error
            "swr_step", "swr_exact_step", "swr_decode_state",
            "swr_uniform_forward", "swr_uniform_backward", "swr_uniform_launch_info",
            "swr_forward_shared_gates", "swr_backward_shared_gates", "swr_shared_gates_workspace_bytes",
-           "SWRFunction", "SWRUniformFunction", "SWRSharedGatesFunction", "library_path", "load"]
+           "SWRFunction", "SWRUniformFunction", "SWRSharedGatesFunction", "library_path", "load",
+           "swr_rms_norm", "swr_rms_norm_backward", "swr_fp4_pack", "swr_fp4_linear", "swr_block_tables",
+           "swr_cache_append", "swr_paged_attention", "SWRNormFunction"]
 
 SWR_ABI_VERSION = 1
 SWR_DTYPE_F32 = 0
@@ -864,4 +866,11 @@ def __getattr__(name):
         if _FUNCTIONS is None:
             _FUNCTIONS = dict(zip(names, _autograd_function()))
         return _FUNCTIONS[name]
+    if name == "SWRNormFunction":
+        return hybrid.SWRNormFunction
     raise AttributeError(name)
+
+
+from . import hybrid  # noqa: E402  (it marshals with the functions above)
+from .hybrid import (swr_block_tables, swr_cache_append, swr_fp4_linear, swr_fp4_pack,  # noqa: E402
+                     swr_paged_attention, swr_rms_norm, swr_rms_norm_backward)

@@ -18,10 +18,12 @@ LIB = os.path.join(HERE, "libswr.so")
 BINDING = os.path.join(HERE, "_binding.so")
 BINDING_SOURCE = os.path.join(CSRC, "swr_binding.cpp")
 ABI_HEADER = os.path.join(os.path.dirname(HERE), "include", "swr.h")
+HYBRID_HEADER = os.path.join(os.path.dirname(HERE), "include", "swr_hybrid.h")
 SOURCES = [os.path.join(CSRC, n) for n in ("swr_api.cpp", "swr_kernels.hip", "swr_uniform.hip", "swr_groups.hip",
-                                            "swr_noalloc.hip", "swr_chain.hip")]
+                                            "swr_noalloc.hip", "swr_chain.hip", "swr_hybrid_api.cpp", "swr_norm.hip",
+                                            "swr_fp4.hip", "swr_paged.hip")]
 HEADERS = [os.path.join(CSRC, "swr_launch.h"), os.path.join(CSRC, "swr_device.h"),
-           os.path.join(CSRC, "swr_internal.h"), ABI_HEADER]
+           os.path.join(CSRC, "swr_internal.h"), os.path.join(CSRC, "swr_hybrid_launch.h"), ABI_HEADER, HYBRID_HEADER]
 ARCH = "gfx950"
 
 
