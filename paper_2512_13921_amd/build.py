@@ -89,11 +89,11 @@ def _temporary(out: str) -> str:
 
 
 def binding_key() -> str:
-    """What the binding's extension module depends on: its source, the C ABI,
+    """What the binding's extension module depends on: its source, the C ABI's headers,
     and the Python and torch that it is compiled against."""
     import torch
     key = hashlib.sha256(f"{sys.version} {torch.__version__}".encode())
-    for path in (BINDING_SOURCE, ABI_HEADER):
+    for path in (BINDING_SOURCE, ABI_HEADER, HYBRID_HEADER):
         with open(path, "rb") as f:
             key.update(f.read())
     return key.hexdigest()

@@ -19,6 +19,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/swr.h"
+#include "../../include/swr_hybrid.h"
 
 // What this module was built from and for; the build looks for it in the file.
 extern "C" __attribute__((used)) const char swr_binding_key[] = "swr-binding-key:" SWR_BINDING_KEY;
@@ -47,6 +48,23 @@ union {
     void* address[kEntries];
 } abi;
 
+// Those of the hybrid model's operators.
+struct HybridAbi {
+    decltype(&swr_rms_norm) rms_norm;
+    decltype(&swr_rms_norm_workspace_bytes) rms_norm_workspace_bytes;
+    decltype(&swr_rms_norm_backward) rms_norm_backward;
+    decltype(&swr_fp4_linear) fp4_linear;
+    decltype(&swr_block_tables) block_tables;
+    decltype(&swr_cache_append) cache_append;
+    decltype(&swr_paged_workspace_bytes) paged_workspace_bytes;
+    decltype(&swr_paged_attention) paged_attention;
+};
+constexpr int kHybridEntries = sizeof(HybridAbi) / sizeof(void*);
+union {
+    HybridAbi fn;
+    void* address[kHybridEntries];
+} hybrid;
+
 // Arguments of one call, taken in order; ok turns false at the first that is
 // not what the fast path handles.
 struct Args {
@@ -73,6 +91,11 @@ struct Args {
         return r;
     }
     bool truth() { return *v++ == Py_True; }
+    double real() {
+        PyObject* o = *v++;
+        if (!PyFloat_Check(o)) { ok = false; return 0; }
+        return PyFloat_AS_DOUBLE(o);
+    }
 };
 
 bool same_layout(const at::Tensor& x, const at::Tensor& t) {
@@ -408,6 +431,247 @@ PyObject* backward_shared_gates(PyObject*, PyObject* const* v, Py_ssize_t) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---------------------------------------------------------------------------
+// The hybrid model's operators
+// ---------------------------------------------------------------------------
+
+bool float_or_bf16(const at::Tensor& t) { return t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kFloat; }
+int code_of(const at::Tensor& t) { return t.scalar_type() == at::kBFloat16 ? SWR_DTYPE_BF16 : SWR_DTYPE_F32; }
+bool is(const at::Tensor& t, const at::Tensor& x, at::ScalarType type, at::IntArrayRef shape) {
+    return t.scalar_type() == type && t.device() == x.device() && t.sizes() == shape;
+}
+bool dense(const at::Tensor& t, const at::Tensor& x, at::ScalarType type, at::IntArrayRef shape) {
+    return is(t, x, type, shape) && t.is_contiguous();
+}
+at::Tensor made(const at::Tensor& x, at::IntArrayRef shape, at::ScalarType type) {
+    return at::empty(shape, x.options().dtype(type).requires_grad(false));
+}
+
+// Rows of t: [width], [rows, width] or [outer, inner, width], channels contiguous
+// (others go through Python).
+bool rows(const at::Tensor& t, int64_t* outer, int64_t* inner, int64_t* so, int64_t* si) {
+    const int64_t d = t.dim();
+    if (d < 1 || d > 3 || (t.stride(d - 1) != 1 && t.size(d - 1) > 1)) return false;
+    *outer = d == 3 ? t.size(0) : 1;
+    *inner = d > 1 ? t.size(d - 2) : 1;
+    *so = d == 3 ? t.stride(0) : 0;
+    *si = d > 1 ? t.stride(d - 2) : 0;
+    return true;
+}
+
+bool norm_problem(const at::Tensor& x, const at::Tensor& w, double eps, swr_norm_t* n) {
+    *n = swr_norm_t{};
+    if (!x.is_cuda() || !float_or_bf16(x) || !rows(x, &n->outer, &n->inner, &n->sx_o, &n->sx_i)) return false;
+    if (w.device() != x.device() || !float_or_bf16(w) || w.dim() != 1 || w.size(0) != x.size(-1) || !w.is_contiguous())
+        return false;
+    n->abi_version = SWR_ABI_VERSION;
+    n->dtype = n->out_dtype = code_of(x);
+    n->weight_dtype = code_of(w);
+    n->width = x.size(-1);
+    n->eps = (float)eps;
+    return true;
+}
+// Row strides of t, which has x's shape, type and device.
+bool norm_rows(const at::Tensor& x, const at::Tensor& t, int64_t* so, int64_t* si) {
+    int64_t outer, inner;
+    return is(t, x, x.scalar_type(), x.sizes()) && rows(t, &outer, &inner, so, si);
+}
+// ... of a contiguous one
+void dense_rows(const swr_norm_t& n, int64_t* so, int64_t* si) {
+    *so = n.inner * n.width;
+    *si = n.width;
+}
+
+// rms_norm(x, weight, residual, eps, fp8, stream) -> (y, scale, h)
+PyObject* rms_norm(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    const at::Tensor &x = g.tensor(), &w = g.tensor();
+    const at::Tensor r = g.optional();
+    const double eps = g.real();
+    const bool fp8 = g.truth();
+    swr_norm_t n;
+    if (!g.ok || !norm_problem(x, w, eps, &n) || (r.defined() && !norm_rows(x, r, &n.sr_o, &n.sr_i))) return none();
+    void* st = stream_of(*g.v, x, &g.ok);
+    if (!g.ok) return none();
+    if (fp8) n.out_dtype = SWR_DTYPE_FP8;
+    dense_rows(n, &n.sy_o, &n.sy_i);
+    dense_rows(n, &n.sh_o, &n.sh_i);
+    at::Tensor y, s, h;
+    int rc;
+    {
+        const Unlocked unlocked;
+        y = made(x, x.sizes(), fp8 ? at::kFloat8_e4m3fn : x.scalar_type());
+        if (fp8) s = made(x, x.sizes().slice(0, x.dim() - 1), at::kFloat);
+        if (r.defined()) h = made(x, x.sizes(), x.scalar_type());
+        rc = hybrid.fn.rms_norm(&n, ptr(x), ptr(r), ptr(w), ptr(y), fptr(s), ptr(h), st);
+    }
+    return results(rc, {y, s, h});
+    END_HANDLE_TH_ERRORS
+}
+
+// rms_norm_backward(h, weight, dy, dh, eps, stream) -> (dx, dweight)
+PyObject* rms_norm_backward(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    const at::Tensor &h = g.tensor(), &w = g.tensor(), &dy = g.tensor();
+    const at::Tensor dh = g.optional();
+    const double eps = g.real();
+    swr_norm_t n;
+    if (!g.ok || !norm_problem(h, w, eps, &n) || !norm_rows(h, dy, &n.sy_o, &n.sy_i) ||
+        (dh.defined() && !norm_rows(h, dh, &n.sr_o, &n.sr_i)))
+        return none();
+    void* st = stream_of(*g.v, h, &g.ok);
+    if (!g.ok) return none();
+    dense_rows(n, &n.sh_o, &n.sh_i);
+    const int64_t ws = hybrid.fn.rms_norm_workspace_bytes(&n);
+    if (ws < 0) return none();
+    const at::Tensor work = workspace(h, std::max<int64_t>(ws / 4, 4), *g.v, st);
+    at::Tensor dx, dw;
+    int rc;
+    {
+        const Unlocked unlocked;
+        dx = made(h, h.sizes(), h.scalar_type());
+        dw = made(h, w.sizes(), at::kFloat);
+        rc = hybrid.fn.rms_norm_backward(&n, ptr(h), ptr(w), ptr(dy), ptr(dh), ptr(dx), fptr(dw), ptr(work), st);
+    }
+    return results(rc, {dx, dw});
+    END_HANDLE_TH_ERRORS
+}
+
+bool matrix(const at::Tensor& t) { return t.dim() == 2 && (t.stride(1) == 1 || t.size(1) <= 1); }
+
+// fp4_linear(x, codes, powers, scale, stream) -> y, x a matrix
+PyObject* fp4_linear(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    const at::Tensor &x = g.tensor(), &c = g.tensor(), &e = g.tensor();
+    const at::Tensor s = g.optional();
+    const bool fp8 = x.defined() && x.scalar_type() == at::kFloat8_e4m3fn;
+    if (!g.ok || !x.is_cuda() || !matrix(x) || !(fp8 || float_or_bf16(x)) || !matrix(c) || !matrix(e)) return none();
+    void* st = stream_of(*g.v, x, &g.ok);
+    swr_fp4_t p = {};
+    p.abi_version = SWR_ABI_VERSION;
+    p.M = x.size(0); p.K = x.size(1); p.N = c.size(0);
+    const int64_t groups = (p.K + 31) / 32;
+    if (!g.ok || !is(c, x, at::kByte, {p.N, 16 * groups}) || !is(e, x, at::kByte, {p.N, groups}) ||
+        (s.defined() && !dense(s, x, at::kFloat, {p.M})))
+        return none();
+    p.dtype = fp8 ? SWR_DTYPE_FP8 : code_of(x);
+    p.out_dtype = fp8 ? SWR_DTYPE_BF16 : p.dtype;
+    p.sx = x.stride(0); p.sy = p.N; p.sc = c.stride(0); p.sp = e.stride(0);
+    at::Tensor y;
+    int rc;
+    {
+        const Unlocked unlocked;
+        y = made(x, {p.M, p.N}, fp8 ? at::kBFloat16 : x.scalar_type());
+        rc = hybrid.fn.fp4_linear(&p, ptr(x), fptr(s), ptr(c), ptr(e), ptr(y), st);
+    }
+    return results(rc, {y});
+    END_HANDLE_TH_ERRORS
+}
+
+// block_tables(lengths, new_tokens, table, stack, count, page_size, tokens, stream)
+//     -> (slots, starts, new_lengths, new_count)
+PyObject* block_tables(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    const at::Tensor &n = g.tensor(), &more = g.tensor(), &table = g.tensor(), &stack = g.tensor(), &count = g.tensor();
+    swr_tables_t p = {};
+    p.page_size = g.integer();
+    p.tokens = g.integer();
+    if (!g.ok || !n.is_cuda() || n.dim() != 1 || stack.dim() != 1 || !matrix(table) || p.tokens < 0) return none();
+    void* st = stream_of(*g.v, n, &g.ok);
+    p.abi_version = SWR_ABI_VERSION;
+    p.batch = n.size(0); p.max_pages = table.size(1); p.st = table.stride(0); p.free_pages = stack.size(0);
+    if (!g.ok || !dense(n, n, at::kInt, {p.batch}) || !dense(more, n, at::kInt, {p.batch}) ||
+        !is(table, n, at::kInt, {p.batch, p.max_pages}) || !dense(stack, n, at::kInt, {p.free_pages}) ||
+        !is(count, n, at::kInt, {1}))
+        return none();
+    at::Tensor slots, starts, lengths, left;
+    int rc;
+    {
+        const Unlocked unlocked;
+        slots = made(n, {p.tokens}, at::kLong);
+        starts = made(n, {p.batch + 1}, at::kInt);
+        lengths = made(n, {p.batch}, at::kInt);
+        left = made(n, {1}, at::kInt);
+        rc = hybrid.fn.block_tables(&p, (const int32_t*)ptr(n), (const int32_t*)ptr(more), (const int32_t*)ptr(stack),
+                                    (const int32_t*)ptr(count), (int32_t*)ptr(table), (int64_t*)ptr(slots),
+                                    (int32_t*)ptr(starts), (int32_t*)ptr(lengths), (int32_t*)ptr(left), st);
+    }
+    return results(rc, {slots, starts, lengths, left});
+    END_HANDLE_TH_ERRORS
+}
+
+bool cache_problem(const at::Tensor& k, const at::Tensor& v, swr_cache_t* c) {
+    if (!k.is_cuda() || k.dim() != 4 || !float_or_bf16(k) || !same_layout(k, v) || (k.stride(3) != 1 && k.size(3) > 1))
+        return false;
+    c->abi_version = SWR_ABI_VERSION;
+    c->dtype = code_of(k);
+    c->pages = k.size(0); c->page_size = k.size(1); c->heads = k.size(2); c->D = k.size(3);
+    c->s_page = k.stride(0); c->s_token = k.stride(1); c->s_head = k.stride(2);
+    return true;
+}
+bool head_rows(const at::Tensor& t, const at::Tensor& cache, at::IntArrayRef shape) {
+    return is(t, cache, cache.scalar_type(), shape) && (t.stride(2) == 1 || t.size(2) <= 1);
+}
+
+// cache_append(k, v, k_cache, v_cache, slots, stream) -> True
+PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{a};
+    const at::Tensor &k = g.tensor(), &v = g.tensor(), &kc = g.tensor(), &vc = g.tensor(), &slots = g.tensor();
+    swr_cache_t c;
+    if (!g.ok || !cache_problem(kc, vc, &c) || slots.dim() != 1) return none();
+    void* st = stream_of(*g.v, kc, &g.ok);
+    const int64_t tokens = slots.size(0);
+    const std::array<int64_t, 3> shape{tokens, c.heads, c.D};
+    if (!g.ok || !dense(slots, kc, at::kLong, {tokens}) || !head_rows(k, kc, shape) || !head_rows(v, kc, shape))
+        return none();
+    const int64_t sk[2] = {k.stride(0), k.stride(1)}, sv[2] = {v.stride(0), v.stride(1)};
+    const int rc = call(hybrid.fn.cache_append, &c, tokens, sk, sv, ptr(k), ptr(v), (const int64_t*)ptr(slots), ptr(kc),
+                        ptr(vc), st);
+    if (rc != 0) return PyLong_FromLong(rc);
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
+// paged_attention(q, k_cache, v_cache, table, lengths, scale, window, want_lse, stream) -> (y, lse)
+PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{a};
+    const at::Tensor &q = g.tensor(), &kc = g.tensor(), &vc = g.tensor(), &table = g.tensor(), &n = g.tensor();
+    const double scale = g.real();
+    swr_paged_t p = {};
+    p.window = g.integer();
+    const bool want = g.truth();
+    if (!g.ok || !cache_problem(kc, vc, &p.cache) || q.dim() != 3 || !matrix(table)) return none();
+    void* st = stream_of(*g.v, kc, &g.ok);
+    p.batch = q.size(0); p.q_heads = q.size(1); p.max_pages = table.size(1); p.st = table.stride(0);
+    if (!g.ok || p.cache.heads < 1 || p.q_heads < 1 || p.q_heads % p.cache.heads != 0 ||
+        !head_rows(q, kc, {p.batch, p.q_heads, p.cache.D}) || !is(table, kc, at::kInt, {p.batch, p.max_pages}) ||
+        !dense(n, kc, at::kInt, {p.batch}))
+        return none();
+    p.sq_b = q.stride(0); p.sq_h = q.stride(1);
+    p.sy_b = p.q_heads * p.cache.D; p.sy_h = p.cache.D;
+    p.scale = (float)scale;
+    const int64_t ws = hybrid.fn.paged_workspace_bytes(&p);
+    if (ws < 0) return none();
+    const at::Tensor work = workspace(q, std::max<int64_t>(ws / 4, 4), *g.v, st);
+    at::Tensor y, lse;
+    int rc;
+    {
+        const Unlocked unlocked;
+        y = made(q, q.sizes(), q.scalar_type());
+        if (want) lse = made(q, {p.batch, p.q_heads}, at::kFloat);
+        rc = hybrid.fn.paged_attention(&p, ptr(q), ptr(kc), ptr(vc), (const int32_t*)ptr(table), (const int32_t*)ptr(n),
+                                       ptr(y), fptr(lse), ptr(work), st);
+    }
+    return results(rc, {y, lse});
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(address, ...): the C ABI's entry points, in Abi's order
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
     if (n != kEntries) {
@@ -419,10 +683,23 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+// bind_hybrid(address, ...): those of the hybrid model's operators, in HybridAbi's order
+PyObject* bind_hybrid(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    if (n != kHybridEntries) {
+        PyErr_SetString(PyExc_TypeError, "bind_hybrid: wrong number of entry points");
+        return nullptr;
+    }
+    for (int i = 0; i < kHybridEntries; ++i) hybrid.address[i] = PyLong_AsVoidPtr(v[i]);
+    if (PyErr_Occurred()) return nullptr;
+    Py_RETURN_NONE;
+}
+
 #define ENTRY(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(bind), ENTRY(forward), ENTRY(backward), ENTRY(exact_forward), ENTRY(exact_backward),
                          ENTRY(step), ENTRY(decode_state), ENTRY(uniform_forward), ENTRY(uniform_backward),
-                         ENTRY(forward_shared_gates), ENTRY(backward_shared_gates), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(forward_shared_gates), ENTRY(backward_shared_gates), ENTRY(bind_hybrid),
+                         ENTRY(rms_norm), ENTRY(rms_norm_backward), ENTRY(fp4_linear), ENTRY(block_tables),
+                         ENTRY(cache_append), ENTRY(paged_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -5,14 +5,17 @@ The normed residual stream (``swr_rms_norm``), the projections of decoded
 tokens with 4-bit weights (``swr_fp4_pack``, ``swr_fp4_linear``) and the
 attention layers over a paged key-value cache (``swr_block_tables``,
 ``swr_cache_append``, ``swr_paged_attention``).  The functions marshal torch
-tensors into pointers, strides and the current HIP stream; every step of the
-computation runs in the library's HIP kernels.  There is no CPU fallback.
+tensors into pointers, strides and the current HIP stream, the ordinary call in
+native code (``csrc/swr_binding.cpp``); every step of the computation runs in
+the library's HIP kernels.  There is no CPU fallback.
 """
 import ctypes
 import math
 
-from . import (SWR_ABI_VERSION, SWR_DTYPE_BF16, SWR_DTYPE_F32, SwrError, _on, _opt, _ptr, _raw, _stream, _torch,
-               load)
+import paper_2512_13921_amd as _package
+
+from . import (SWR_ABI_VERSION, SWR_DTYPE_BF16, SWR_DTYPE_F32, SwrError, _checked, _on, _opt, _ptr, _raw, _stream,
+               _torch, load)
 
 __all__ = ["swr_rms_norm", "swr_rms_norm_backward", "swr_fp4_pack", "swr_fp4_linear", "swr_block_tables",
            "swr_cache_append", "swr_paged_attention", "SWRNormFunction"]
@@ -74,6 +77,23 @@ def _lib():
             entry.restype, entry.argtypes = restype, args
         _bound = lib
     return lib
+
+
+# The entry points that the native marshalling calls, in its order.
+_BOUND = ("swr_rms_norm", "swr_rms_norm_workspace_bytes", "swr_rms_norm_backward", "swr_fp4_linear",
+          "swr_block_tables", "swr_cache_append", "swr_paged_workspace_bytes", "swr_paged_attention")
+_native = None   # (the package's native marshalling, the library that it is bound to)
+
+
+def _fast():
+    """The native marshalling, bound to the loaded library's entry points."""
+    global _native
+    module = _package._fast()
+    if _native is None or _native[0] is not module or _native[1] is not _bound:
+        lib = _lib()
+        module.bind_hybrid(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in _BOUND))
+        _native = (module, lib)
+    return module
 
 
 def _check(rc, what):
@@ -172,6 +192,13 @@ def swr_rms_norm(x, weight, residual=None, eps=1e-6, fp8=False, y=None, h=None, 
     Returns y; with a ``residual`` (or an ``h`` to fill) (y, h); with ``fp8``, y is a
     ``float8_e4m3fn`` tensor q followed by its rows' float32 scales: (q, scale)
     or (q, scale, h).  ``h`` may be x or residual itself (updated in place)."""
+    if y is None and h is None:
+        r = _fast().rms_norm(x, weight, residual, eps, bool(fp8), _raw(stream))
+        if r is not None:
+            y, scale, h = _checked(r, "swr_rms_norm")
+            if h is None:
+                return (y, scale) if fp8 else y
+            return (y, scale, h) if fp8 else (y, h)
     torch = _torch()
     n = _norm(x, weight, eps, SWR_DTYPE_FP8 if fp8 else None)
     if residual is not None:
@@ -198,6 +225,10 @@ def swr_rms_norm_backward(h, weight, dy, dh=None, eps=1e-6, dx=None, dweight=Non
     """(dx, dweight) of ``swr_rms_norm`` at its sum h, given dy and the gradient
     dh (or None) that reaches h on its other ways.  dx is the gradient of x and of the
     residual alike (it may be dy or dh itself); dweight is float32."""
+    if dx is None and dweight is None and workspace is None:
+        r = _fast().rms_norm_backward(h, weight, dy, dh, eps, _raw(stream))
+        if r is not None:
+            return _checked(r, "swr_rms_norm_backward")
     torch = _torch()
     n = _norm(h, weight, eps, None)
     n.sy_o, n.sy_i = _same(h, dy, "dy")
@@ -251,6 +282,10 @@ def swr_fp4_linear(x, codes, powers, scale=None, out_dtype=None, y=None, stream=
     """y = x W^T of rows x [.., K] (float32, bfloat16, or ``float8_e4m3fn``) with
     packed weights W [N, K], times ``scale`` [..] (float32, a factor per row)
     where given.  y is in ``out_dtype``: x's by default, bfloat16 for 8-bit rows."""
+    if y is None and out_dtype is None:
+        r = _fast().fp4_linear(x, codes, powers, scale, _raw(stream))
+        if r is not None:
+            return _checked(r, "swr_fp4_linear")
     torch = _torch()
     _gpu(x, "x")
     p = SwrFp4()
@@ -294,6 +329,11 @@ def swr_block_tables(lengths, new_tokens, block_table, free_stack, free_count, p
     the new tokens' slots in the cache (int64 [tokens]; -1 for none), the first
     of each request's (int32 [batch + 1]), the requests' new lengths, and the
     free pages left.  ``tokens`` is the number of new tokens, or a bound on it."""
+    if slots is None and starts is None and new_lengths is None and new_free_count is None:
+        r = _fast().block_tables(lengths, new_tokens, block_table, free_stack, free_count, page_size, tokens,
+                                 _raw(stream))
+        if r is not None:
+            return _checked(r, "swr_block_tables")
     torch = _torch()
     i32 = torch.int32
     _gpu(lengths, "lengths")
@@ -349,6 +389,10 @@ def swr_cache_append(k, v, k_cache, v_cache, slots, stream=None):
     """New keys and values, [tokens, heads, D], into their ``slots`` (int64
     [tokens]) of a layer's cache [pages, page_size, heads, D], in place.  A token
     whose slot is not within the cache is left out."""
+    r = _fast().cache_append(k, v, k_cache, v_cache, slots, _raw(stream))
+    if r is not None:
+        _checked(r, "swr_cache_append")
+        return
     torch = _torch()
     c = SwrCache()
     _cache(c, k_cache, v_cache)
@@ -368,6 +412,13 @@ def swr_paged_attention(q, k_cache, v_cache, block_table, lengths, scale=None, w
     ``lengths`` [batch] cached tokens (see ``include/swr_hybrid.h``); the last ``window`` of them
     where that is not 0.  ``scale`` is 1 / sqrt(D) by default.  Returns y, or
     (y, lse) with the logarithms of the softmax sums, float32 [batch, q_heads]."""
+    if y is None and workspace is None and q.dim() == 3:
+        r = _fast().paged_attention(q, k_cache, v_cache, block_table, lengths,
+                                    q.shape[2] ** -0.5 if scale is None else scale, window, bool(want_lse),
+                                    _raw(stream))
+        if r is not None:
+            y, lse = _checked(r, "swr_paged_attention")
+            return (y, lse) if want_lse else y
     torch = _torch()
     p = SwrPaged()
     _cache(p.cache, k_cache, v_cache)
