@@ -221,7 +221,7 @@ int swr_rms_norm_backward(const swr_norm_t* n, const void* h, const void* weight
     swr::NormParams p = norm_params(n, r);
     p.dw = dweight;
     if (r.empty)   // no row: dweight is a sum of nothing
-        return status(swr::launch_norm_backward(*n, swr::NormPlan{0, 0, 0}, p, stream));
+        return status(swr::launch_norm_backward(*n, swr::NormPlan{false, 0, 0, 0}, p, stream));
     if (!h || !weight || !dy || !dx || !workspace) return SWR_ERR_NULL;
     if (!aligned(h, r.es) || !aligned(dy, r.es) || !aligned(dh, r.es) || !aligned(dx, r.es) ||
         !aligned(weight, size_of(n->weight_dtype)) || !aligned(workspace, 16))

@@ -28,10 +28,12 @@ struct NormParams {
     int64_t sx_o, sx_i, sr_o, sr_i, sh_o, sh_i, sy_o, sy_i;
 };
 
-// How a norm launch covers its rows: tpr threads a row, each with vpt 16-byte
-// vectors of it in registers (vpt = 0: rows too wide for that, walked twice).
+// How a norm launch covers its rows: a row by a wave (blocks of four) or by a
+// block of its own, vpt 16-byte vectors of it in a thread's registers (vpt = 0:
+// rows too wide for that, walked twice).
 struct NormPlan {
-    int tpr, vpt;
+    bool block;
+    int vpt, threads;
     int blocks;          // backward: workgroups, each with a share of dw
 };
 NormPlan plan_norm(int dtype, int64_t rows, int64_t width, bool backward);
