@@ -205,7 +205,8 @@ int swr_paged_attention(const swr_paged_t* p, const void* q, const void* k_cache
                         const int32_t* table, const int32_t* lengths, void* y, float* lse, void* workspace,
                         void* stream);
 
-/* Bytes of workspace that swr_paged_attention needs (16-byte aligned), or an SWR_ERR_* code. */
+/* Bytes of workspace that swr_paged_attention needs (16-byte aligned; it may be
+ * NULL where they are 0), or an SWR_ERR_* code. */
 int64_t swr_paged_workspace_bytes(const swr_paged_t* p);
 
 #ifdef __cplusplus

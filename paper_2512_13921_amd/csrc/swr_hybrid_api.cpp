@@ -425,7 +425,7 @@ int64_t swr_paged_workspace_bytes(const swr_paged_t* p) {
     const int rc = resolve_paged(p, &cache, &q, &y);
     if (rc != SWR_OK) return rc;
     if (p->batch == 0) return 0;
-    return (int64_t)swr::paged_workgroups(*p) * 2 * swr::paged_part_floats(*p) * 4;
+    return swr::paged_work_floats(*p) * 4;
 }
 
 int swr_paged_attention(const swr_paged_t* p, const void* q, const void* k_cache, const void* v_cache,
@@ -436,11 +436,12 @@ int swr_paged_attention(const swr_paged_t* p, const void* q, const void* k_cache
     if (rc != SWR_OK) return rc;
     if (p->batch == 0) return SWR_OK;
     const bool cached = p->cache.pages > 0 && p->max_pages > 0;
-    if (!q || !y || !lengths || !workspace || (cached && (!k_cache || !v_cache || !table))) return SWR_ERR_NULL;
+    const int64_t work = swr::paged_work_floats(*p) * 4;
+    if (!q || !y || !lengths || (work > 0 && !workspace)) return SWR_ERR_NULL;
+    if (cached && (!k_cache || !v_cache || !table)) return SWR_ERR_NULL;
     if (!aligned(q, 16) || !aligned(y, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(table, 4) ||
         !aligned(lengths, 4) || !aligned(lse, 4) || !aligned(workspace, 16))
         return SWR_ERR_ALIGN;
-    const int64_t work = (int64_t)swr::paged_workgroups(*p) * 2 * swr::paged_part_floats(*p) * 4;
     const int64_t cells = (max_offset({{p->batch, p->st}, {p->max_pages, 1}}) + 1) * 4;
     const Span in[5] = {span(q, bq), span(k_cache, bc), span(v_cache, bc), span(cached ? table : nullptr, cells),
                         span(lengths, p->batch * 4)};
@@ -454,16 +455,17 @@ int swr_paged_attention(const swr_paged_t* p, const void* q, const void* k_cache
     const int64_t unit = 16 / size_of(p->cache.dtype);
     swr::PagedParams a = {};
     a.q = q; a.k = k_cache; a.v = v_cache; a.table = table; a.lengths = lengths; a.y = y; a.lse = lse;
-    a.part = (float*)workspace;
     a.batch = (int32_t)p->batch;
     a.kv_heads = (int32_t)p->cache.heads;
     a.group = (int32_t)(p->q_heads / p->cache.heads);
     a.head_tiles = (a.group + 15) / 16;
     a.D = (int32_t)p->cache.D;
     a.max_pages = p->cache.pages > 0 ? (int32_t)p->max_pages : 0;   // (no page: no position)
-    a.page_size = (int32_t)p->cache.page_size;
+    a.page = swr::Divisor(p->cache.page_size);
     a.pages = (int32_t)p->cache.pages;
     a.workgroups = swr::paged_workgroups(*p);
+    a.cuts = (int32_t*)workspace;
+    a.part = (float*)workspace + 4 * (int64_t)a.workgroups;
     a.st = p->st;
     a.window = p->window;
     a.sq_b = p->sq_b; a.sq_h = p->sq_h; a.sy_b = p->sy_b; a.sy_h = p->sy_h;

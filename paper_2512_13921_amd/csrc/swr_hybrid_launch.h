@@ -53,6 +53,22 @@ hipError_t launch_fp4(int dtype, int out_dtype, const Fp4Params& p, void* stream
 hipError_t launch_fp4_pack(int dtype, const void* w, int64_t N, int64_t K, int64_t sw, uint8_t* codes, uint8_t* powers,
                            int64_t sc, int64_t sp, void* stream);
 
+// Division of whole numbers below 2^31 by d (1 to 65536) with a multiplication:
+// with L = ceil(log2 d) and m = floor(2^(31 + L) / d) + 1 < 2^32, n m exceeds
+// n 2^(31 + L) / d by less than 2^(31 + L) / d.
+struct Divisor {
+    uint32_t d, m, shift;   // m = 0: d is 1
+    Divisor() = default;
+    explicit Divisor(int64_t by) : d((uint32_t)by), m(0), shift(0) {
+        if (by <= 1) return;
+        uint32_t L = 0;
+        while (((int64_t)1 << L) < by) ++L;
+        m = (uint32_t)(((uint64_t)1 << (31 + L)) / d + 1);
+        shift = L - 1;
+    }
+    __device__ uint32_t over(uint32_t n) const { return m ? __umulhi(n, m) >> shift : n; }
+};
+
 struct TableParams {
     const int32_t *lengths, *news, *stack, *count;
     int32_t* table;
@@ -81,19 +97,21 @@ struct PagedParams {
     const int32_t *table, *lengths;
     void* y;
     float* lse;
-    float* part;                         // shares of split rows: [workgroups][2][16][dp + 2]
+    float* part;                         // parts of rows cut between workgroups: [workgroups][2][16][dp + 2]
+    int32_t* cuts;                       // [workgroups][4]: request, head row and parts of such a row
     int32_t batch, kv_heads, group;      // group: query heads that share a key head
     int32_t head_tiles;                  // ceil(group / 16)
-    int32_t D, max_pages, page_size, pages;
-    int32_t workgroups;
+    int32_t D, max_pages, pages;
+    Divisor page;                        // by the page size
+    int32_t workgroups;                  // among which the tiles are shared out; 0: a workgroup a row
     int64_t st, window;
     int64_t sq_b, sq_h, sy_b, sy_h;      // elements
     uint32_t s_page, s_token, s_head;    // 16-byte units
     float scale_log2;                    // scale * log2(e)
 };
-// Workgroups (and with them shares) that the attention's launch uses at most.
+// Workgroups that share out the attention's work (0: a workgroup a row).
 int paged_workgroups(const swr_paged_t& p);
-int64_t paged_part_floats(const swr_paged_t& p);
+int64_t paged_work_floats(const swr_paged_t& p);
 hipError_t launch_paged(int dtype, const PagedParams& p, void* stream);
 
 }  // namespace swr

@@ -143,12 +143,19 @@ __global__ __launch_bounds__(256) void swr_append_kernel(AppendParams p) {
 // end and cut into equal shares, one a workgroup: every workgroup finds its own share
 // from the lengths, so a long request among short ones costs no idle
 // workgroups, and no host knows the lengths.  Waves take a row's tiles in turn
-// and are joined in LDS.  A row cut between workgroups leaves its
-// parts in the workspace, which swr_paged_join_kernel joins.
+// and are joined in LDS.  A row cut between workgroups leaves its parts
+// in the workspace, which swr_paged_join_kernel joins.
 
 constexpr int kTile = 32;      // tokens of a wave's tile
 constexpr int kWaves = 4;
-constexpr uint32_t kNoRow = 0xffffffffu;
+constexpr int kShort = 1024;   // positions up to which a row is one block's
+// Shares of the work: three workgroups a compute unit, which is what a unit
+// holds of heads of up to 256 bytes.  Not a power of two: of equal rows, whose
+// lengths mostly are, shares would begin at multiples of large powers of two and so
+// on few of the memory's channels (2 requests of 262147 tokens, 16 heads of 64, bf16: 512
+// shares 492 us, 768 410, 1024 482; 8 heads of 128: 408, 374, 398).
+constexpr int kShares = 768;
+constexpr int kRowCost = 4;
 
 // Tiles and first position of request b.
 struct Rows {
@@ -156,41 +163,45 @@ struct Rows {
     int tiles, length;
 };
 __device__ inline Rows rows_of(const PagedParams& p, int b) {
-    const int64_t most = (int64_t)p.max_pages * p.page_size;
+    const int64_t most = (int64_t)p.max_pages * p.page.d;
     const int64_t n = max(p.lengths[b], 0), low = p.window > 0 ? max(n - p.window, (int64_t)0) : 0;
     const int64_t end = min(n, most);   // (positions past the table are left out)
     return {low, end > low ? (int)((end - low + kTile - 1) / kTile) : 0, (int)end};
 }
 
-// Where the flat order of tiles stands: (request, head row within the request,
-// tile within the row), and the share of each workgroup.
+// The flat order: (request, head row within the request, place within the row).
+// A row takes kRowCost places, in which nothing is done, before its tiles: what
+// beginning and joining a row costs, in tiles, so that shares of many short rows are
+// no longer than others.
 struct Place {
-    int64_t total;   // tiles of all rows
-    int64_t per;     // tiles a workgroup
-    int b;           // the request that holds tile `at`, and the tiles before it
-    int64_t before;
+    int64_t total;   // places of all rows
+    int64_t per;     // places a workgroup
+    int b;           // the request that holds this workgroup's first place
+    int64_t before;  // and the places before that request
 };
+__device__ inline int64_t places(const Rows& r, int heads) {
+    return r.tiles ? (int64_t)(r.tiles + kRowCost) * heads : 0;
+}
 
-// The place of flat tile `at(per)`, found by the whole block; buf holds 6 values.
-template <class At>
-__device__ inline Place find(const PagedParams& p, int heads, int64_t* buf, At at) {
+// Found by the whole block; buf holds 6 values.
+__device__ inline Place find(const PagedParams& p, int heads, int64_t* buf) {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     int64_t sum = 0;
-    for (int b = threadIdx.x; b < p.batch; b += 256) sum += rows_of(p, b).tiles;
+    for (int b = threadIdx.x; b < p.batch; b += 256) sum += places(rows_of(p, b), heads);
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
     if (lane == 0) buf[wave] = sum;
     __syncthreads();
     Place f;
-    f.total = (buf[0] + buf[1] + buf[2] + buf[3]) * heads;
-    f.per = max((f.total + p.workgroups - 1) / p.workgroups, (int64_t)kWaves);
-    const int64_t want = at(f.per);
+    f.total = buf[0] + buf[1] + buf[2] + buf[3];
+    f.per = max((f.total + p.workgroups - 1) / p.workgroups, (int64_t)(kWaves + kRowCost));
+    const int64_t want = blockIdx.x * f.per;
     int64_t before = 0;
     f.b = p.batch;
     f.before = f.total;
     for (int c = 0; c < p.batch && want < f.total; c += 256) {
         const int b = c + (int)threadIdx.x;
-        const int64_t n = b < p.batch ? (int64_t)rows_of(p, b).tiles * heads : 0;
+        const int64_t n = b < p.batch ? places(rows_of(p, b), heads) : 0;
         int64_t s = n;
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
@@ -234,12 +245,12 @@ struct Running {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const float base = top == -INFINITY ? 0.0f : top;   // (nothing yet: weights of 0, not NaN)
-        const float alpha = exp2f(m - base);
+        const float alpha = __builtin_amdgcn_exp2f(m - base);
         m = top;
         float s = 0.0f;
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-            p[t] = exp2f(p[t] - base);
+            p[t] = __builtin_amdgcn_exp2f(p[t] - base);
             s += p[t];
         }
         sum = sum * alpha + s;
@@ -247,16 +258,34 @@ struct Running {
     }
 };
 
-// One wave's state of one row: columns g = l.
-template <class E, int DP>
+// Where a tile's 32 tokens lie: lane i % 32 has token i's row of the cache, in
+// 16-byte units (0 where it has none), and every lane a bit for each that has one.
+struct Spots {
+    uint32_t row, valid;
+    __device__ bool has(int t) const { return valid >> t & 1; }
+};
+constexpr uint32_t kAll = 0xffffffffu;
+
+// One wave's state of one row: columns g = l.  A tile's K and V are loaded (load)
+// and then worked in (use), so that one tile's loads may be on their way while
+// another is worked on.  FULL: D is DP.  Tokens that are not there have the
+// cache's first row loaded in their place, so that the loads stand without
+// branches; their scores are replaced, and V's rows cleared, in the few tiles that
+// have such.
+template <class E, int DP, bool FULL>
 struct State;
 
 // bf16: DP = 32, 64, 128 or 256 channels (D rounded up).  Lane (l, u) holds
 // channels 32 c + 8 u .. + 7 of K's token row l, and channels l * CH .. of V's rows.
-template <int DP>
-struct State<B16, DP> {
+template <int DP, bool FULL>
+struct State<B16, DP, FULL> {
     static constexpr int CH = DP / 16;          // channels of V that a lane holds
     static constexpr int NK = DP / 32;
+    struct Tile {
+        u32x4 k[2][NK];
+        uint32_t v[8][CH / 2];                  // token 16 (t / 4) + 4 u + t % 4
+        uint32_t valid;
+    };
     bf16x8 q[NK];
     f32x4 acc[CH];                              // acc[j]: channels (4 u + i) * CH + j, column l
     Running run;
@@ -265,58 +294,68 @@ struct State<B16, DP> {
 #pragma unroll
         for (int c = 0; c < NK; ++c) {
             u32x4 v{0, 0, 0, 0};
-            if (in && 32 * c + 8 * u < D) v = *(const u32x4*)(qrow + 32 * c + 8 * u);
+            if (in && (FULL || 32 * c + 8 * u < D)) v = *(const u32x4*)(qrow + 32 * c + 8 * u);
             q[c] = __builtin_bit_cast(bf16x8, v);
         }
 #pragma unroll
         for (int j = 0; j < CH; ++j) acc[j] = f32x4{0, 0, 0, 0};
     }
 
-    // 32 tokens: lane i < 32 has token i's row (16-byte units, kNoRow: none).
-    __device__ void tile(const u32x4* kb, const u32x4* vb, uint32_t row, int l, int u, int D, float scale) {
-        u32x4 k[2][NK];
-        uint32_t v[8][CH / 2];
+    __device__ static void load(Tile& x, const u32x4* kb, const u32x4* vb, const Spots& at, int l, int u, int D) {
+        x.valid = at.valid;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const uint32_t r = (uint32_t)__shfl((int)row, 16 * s + l);
+            const u32x4* k = kb + (uint32_t)__shfl((int)at.row, 16 * s + l) + u;
 #pragma unroll
-            for (int c = 0; c < NK; ++c) {
-                k[s][c] = u32x4{0, 0, 0, 0};
-                if (r != kNoRow && 32 * c + 8 * u < D) k[s][c] = kb[(int64_t)r + 4 * c + u];
-            }
+            for (int c = 0; c < NK; ++c) x.k[s][c] = FULL || 32 * c + 8 * u < D ? k[4 * c] : u32x4{0, 0, 0, 0};
         }
-        bool in[8];
+        const bool ok = FULL || l * CH < D;
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-            const uint32_t r = (uint32_t)__shfl((int)row, 16 * (t / 4) + 4 * u + t % 4);
-            in[t] = r != kNoRow;
-            const bool ok = in[t] && l * CH < D;
-            const uint32_t* at = (const uint32_t*)(vb + (int64_t)(in[t] ? r : 0)) + l * (CH / 2);
+            const uint32_t r = (uint32_t)__shfl((int)at.row, 16 * (t / 4) + 4 * u + t % 4);
+            const uint32_t* v = (const uint32_t*)(vb + r) + l * (CH / 2);
             if constexpr (CH == 2) {
-                v[t][0] = ok ? *at : 0;
+                x.v[t][0] = ok ? *v : 0;
             } else if constexpr (CH == 4) {
-                const u32x2 w = ok ? *(const u32x2*)at : u32x2{0, 0};
-                v[t][0] = w[0]; v[t][1] = w[1];
+                const u32x2 w = ok ? *(const u32x2*)v : u32x2{0, 0};
+                x.v[t][0] = w[0]; x.v[t][1] = w[1];
             } else {
 #pragma unroll
                 for (int h = 0; h < CH / 8; ++h) {
-                    const u32x4 w = ok ? *(const u32x4*)(at + 4 * h) : u32x4{0, 0, 0, 0};
+                    const u32x4 w = ok ? *(const u32x4*)(v + 4 * h) : u32x4{0, 0, 0, 0};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[t][4 * h + i] = w[i];
+                    for (int i = 0; i < 4; ++i) x.v[t][4 * h + i] = w[i];
                 }
             }
         }
+    }
+
+    __device__ void use(Tile& x, int u, float scale) {
         float p[8];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            f32x4 x{0, 0, 0, 0};
+            f32x4 d{0, 0, 0, 0};
 #pragma unroll
             for (int c = 0; c < NK; ++c)
-                x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[s][c]), q[c], x, 0, 0, 0);
+                d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.k[s][c]), q[c], d, 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[4 * s + i] = in[4 * s + i] ? x[i] * scale : -INFINITY;
+            for (int i = 0; i < 4; ++i) p[4 * s + i] = d[i] * scale;
+        }
+        if (x.valid != kAll) {
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const bool in = x.valid >> (16 * (t / 4) + 4 * u + t % 4) & 1;
+                if (!in) p[t] = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < CH / 2; ++j)
+                    if (!in) x.v[t][j] = 0;
+            }
         }
         const float alpha = run.weigh(p);
+        if (__any(alpha != 1.0f)) {   // (the maximum seldom moves)
+#pragma unroll
+            for (int j = 0; j < CH; ++j) acc[j] *= alpha;
+        }
         bf16x8 hi, lo;
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
@@ -329,20 +368,25 @@ struct State<B16, DP> {
             u32x4 a;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                a[t] = __builtin_amdgcn_perm(v[2 * t + 1][j / 2], v[2 * t][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+                a[t] = __builtin_amdgcn_perm(x.v[2 * t + 1][j / 2], x.v[2 * t][j / 2],
+                                             j % 2 ? 0x07060302u : 0x05040100u);
             const bf16x8 w = __builtin_bit_cast(bf16x8, a);
-            f32x4 y = acc[j] * alpha;
-            y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, hi, y, 0, 0, 0);
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, lo, y, 0, 0, 0);
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, hi, acc[j], 0, 0, 0);
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, lo, acc[j], 0, 0, 0);
         }
     }
 };
 
 // float32: lane (l, u) holds channels 16 c + 4 u .. + 3 of K's token row l.
-template <int DP>
-struct State<B32, DP> {
+template <int DP, bool FULL>
+struct State<B32, DP, FULL> {
     static constexpr int CH = DP / 16;
     static constexpr int NK = DP / 16;
+    struct Tile {
+        u32x4 k[2][NK];
+        float v[8][CH];
+        uint32_t valid;
+    };
     f32x4 q[NK];
     f32x4 acc[CH];
     Running run;
@@ -351,47 +395,72 @@ struct State<B32, DP> {
 #pragma unroll
         for (int c = 0; c < NK; ++c) {
             q[c] = f32x4{0, 0, 0, 0};
-            if (in && 16 * c + 4 * u < D) q[c] = *(const f32x4*)(qrow + 16 * c + 4 * u);
+            if (in && (FULL || 16 * c + 4 * u < D)) q[c] = *(const f32x4*)(qrow + 16 * c + 4 * u);
         }
 #pragma unroll
         for (int j = 0; j < CH; ++j) acc[j] = f32x4{0, 0, 0, 0};
     }
 
-    __device__ void tile(const u32x4* kb, const u32x4* vb, uint32_t row, int l, int u, int D, float scale) {
-        float p[8];
-        bool in[8];
+    __device__ static void load(Tile& x, const u32x4* kb, const u32x4* vb, const Spots& at, int l, int u, int D) {
+        x.valid = at.valid;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const uint32_t r = (uint32_t)__shfl((int)row, 16 * s + l);
-            f32x4 x{0, 0, 0, 0};
+            const u32x4* k = kb + (uint32_t)__shfl((int)at.row, 16 * s + l) + u;
 #pragma unroll
-            for (int c = 0; c < NK; ++c) {
-                u32x4 k{0, 0, 0, 0};
-                if (r != kNoRow && 16 * c + 4 * u < D) k = kb[(int64_t)r + 4 * c + u];
+            for (int c = 0; c < NK; ++c) x.k[s][c] = FULL || 16 * c + 4 * u < D ? k[4 * c] : u32x4{0, 0, 0, 0};
+        }
+        const bool ok = FULL || l * CH < D;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            const uint32_t r = (uint32_t)__shfl((int)at.row, 16 * (t / 4) + 4 * u + t % 4);
+            const uint32_t* v = (const uint32_t*)(vb + r) + l * CH;
+            if constexpr (CH == 2) {
+                const u32x2 w = ok ? *(const u32x2*)v : u32x2{0, 0};
+                x.v[t][0] = as_float(w[0]); x.v[t][1] = as_float(w[1]);
+            } else {
+#pragma unroll
+                for (int h = 0; h < CH / 4; ++h) {
+                    const u32x4 w = ok ? *(const u32x4*)(v + 4 * h) : u32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x.v[t][4 * h + i] = as_float(w[i]);
+                }
+            }
+        }
+    }
+
+    __device__ void use(Tile& x, int u, float scale) {
+        float p[8];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            f32x4 d{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < NK; ++c)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    x = __builtin_amdgcn_mfma_f32_16x16x4f32(as_float(k[i]), q[c][i], x, 0, 0, 0);
-            }
+                    d = __builtin_amdgcn_mfma_f32_16x16x4f32(as_float(x.k[s][c][i]), q[c][i], d, 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                in[4 * s + i] = (uint32_t)__shfl((int)row, 16 * s + 4 * u + i) != kNoRow;
-                p[4 * s + i] = in[4 * s + i] ? x[i] * scale : -INFINITY;
+            for (int i = 0; i < 4; ++i) p[4 * s + i] = d[i] * scale;
+        }
+        if (x.valid != kAll) {
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const bool in = x.valid >> (16 * (t / 4) + 4 * u + t % 4) & 1;
+                if (!in) p[t] = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < CH; ++j)
+                    if (!in) x.v[t][j] = 0.0f;
             }
         }
         const float alpha = run.weigh(p);
+        if (__any(alpha != 1.0f)) {
 #pragma unroll
-        for (int j = 0; j < CH; ++j) acc[j] *= alpha;
+            for (int j = 0; j < CH; ++j) acc[j] *= alpha;
+        }
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            const uint32_t r = (uint32_t)__shfl((int)row, 16 * (t / 4) + 4 * u + t % 4);
-            const float* at = (const float*)(vb + (int64_t)(in[t] ? r : 0)) + l * CH;
-            float v[CH];
-#pragma unroll
-            for (int j = 0; j < CH; ++j) v[j] = in[t] && l * CH < D ? at[j] : 0.0f;
+        for (int t = 0; t < 8; ++t)
 #pragma unroll
             for (int j = 0; j < CH; ++j)
-                acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j], p[t], acc[j], 0, 0, 0);
-        }
+                acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.v[t][j], p[t], acc[j], 0, 0, 0);
     }
 };
 
@@ -412,162 +481,281 @@ __device__ inline void finish(const PagedParams& p, int b, int64_t head, int c, 
 // Floats of a row part in the workspace: 16 columns of DP channels, maxima, sums.
 constexpr int64_t part_floats(int dp) { return 16 * ((int64_t)dp + 2); }
 
-template <class E, int DP>
-__global__ __launch_bounds__(kWaves * 64) void swr_paged_kernel(PagedParams p) {
+// Tiles t0 + wave, t0 + wave + WAVES, ... up to t1 of the row (request b, head
+// row h) by the block's waves, and their parts joined in LDS.  Whole rows are
+// finished; a part of one goes to `part`.
+template <class E, int DP, int WAVES>
+struct Joined {
+    float m[WAVES][16], sum[WAVES][16];
+    float acc[WAVES][DP][17];   // (17: the lanes' columns fall on different banks)
+};
+
+template <class E, int DP, bool FULL, int WAVES, bool AHEAD>
+__device__ inline void attend(const PagedParams& p, const Rows& r, int b, int h, int t0, int t1, bool whole,
+                              float* part, Joined<E, DP, WAVES>& join) {
     typedef typename E::T T;
-    typedef State<E, DP> S;
+    typedef State<E, DP, FULL> S;
     constexpr int CH = S::CH;
-    __shared__ int64_t buf[6];
-    __shared__ float join_m[kWaves][16], join_s[kWaves][16];
-    __shared__ float join[kWaves][DP][17];   // (17: the lanes' columns fall on different banks)
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, l = lane % 16, u = lane / 16;
-    const int heads = p.kv_heads * p.head_tiles;
-    const Place f = find(p, heads, buf, [&](int64_t per) { return blockIdx.x * per; });
-    int64_t at = blockIdx.x * f.per;
-    const int64_t end = min(at + f.per, f.total);
-    int64_t before = f.before;
-    for (int b = f.b; at < end; ++b) {
-        const Rows r = rows_of(p, b);
-        if (r.tiles == 0) continue;
-        for (int64_t h = (at - before) / r.tiles; h < heads && at < end; ++h) {
-            const int64_t row0 = before + h * r.tiles;   // the row's tiles: row0 .. row0 + r.tiles
-            const int t0 = (int)(at - row0), t1 = (int)min((int64_t)r.tiles, end - row0);
-            const int kv = (int)(h / p.head_tiles), g0 = (int)(h % p.head_tiles) * 16;
-            const int columns = min(p.group - g0, 16);
-            const int64_t head = (int64_t)kv * p.group + g0;
-            S s;
-            s.begin((const T*)p.q + b * p.sq_b + (head + min(l, columns - 1)) * p.sq_h, l < columns, u, p.D);
-            const u32x4* kb = (const u32x4*)p.k + (int64_t)kv * p.s_head;
-            const u32x4* vb = (const u32x4*)p.v + (int64_t)kv * p.s_head;
-            for (int t = t0 + wave; t < t1; t += kWaves) {
-                const int64_t pos = r.low + (int64_t)t * kTile + lane % kTile;
-                uint32_t row = kNoRow;
-                if (pos < r.length) {
-                    const uint32_t page = (uint32_t)pos / (uint32_t)p.page_size;
-                    const int id = p.table[b * p.st + page];
-                    if (id >= 0 && id < p.pages)
-                        row = (uint32_t)id * p.s_page + ((uint32_t)pos - page * p.page_size) * p.s_token;
-                }
-                s.tile(kb, vb, row, l, u, p.D, p.scale_log2);
-            }
-            // The waves' parts, joined.
-            s.run.sum += __shfl_xor(s.run.sum, 16);
-            s.run.sum += __shfl_xor(s.run.sum, 32);
-            __syncthreads();   // (the last row's parts have been read)
-            if (u == 0) { join_m[wave][l] = s.run.m; join_s[wave][l] = s.run.sum; }
-#pragma unroll
-            for (int j = 0; j < CH; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) join[wave][(4 * u + i) * CH + j][l] = s.acc[j][i];
-            __syncthreads();
-            const bool whole = t0 == 0 && t1 == r.tiles;
-            float* part = p.part + (blockIdx.x * 2 + (t0 == 0 && at > blockIdx.x * f.per ? 1 : 0)) * part_floats(DP);
-            for (int e = threadIdx.x; e < columns * DP; e += kWaves * 64) {
-                const int g = e / DP, c = e % DP;
-                float m = -INFINITY;
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) m = fmaxf(m, join_m[w][g]);
-                const float base = m == -INFINITY ? 0.0f : m;
-                float y = 0.0f, sum = 0.0f;
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) {
-                    const float a = exp2f(join_m[w][g] - base);
-                    y += join[w][c][g] * a;
-                    sum += join_s[w][g] * a;
-                }
-                if (whole) {
-                    finish<T>(p, b, head + g, c, m, y, sum);
-                } else {
-                    part[g * (DP + 2) + c] = y;
-                    if (c == 0) { part[g * (DP + 2) + DP] = m; part[g * (DP + 2) + DP + 1] = sum; }
-                }
-            }
-            at = row0 + t1;
+    const int kv = h / p.head_tiles, g0 = h % p.head_tiles * 16, columns = min(p.group - g0, 16);
+    const int64_t head = (int64_t)kv * p.group + g0;
+    const u32x4* kb = (const u32x4*)p.k + (int64_t)kv * p.s_head;
+    const u32x4* vb = (const u32x4*)p.v + (int64_t)kv * p.s_head;
+    const int32_t* table = p.table + b * p.st;
+    // A tile's spots are looked up while the tile before it is worked on.
+    const auto rows_at = [&](int t) {
+        const int64_t pos = r.low + (int64_t)t * kTile + lane % kTile;
+        Spots at{0, 0};
+        bool in = t < t1 && pos < r.length;
+        if (in) {
+            const uint32_t page = p.page.over((uint32_t)pos);
+            const int id = table[page];
+            in = id >= 0 && id < p.pages;
+            if (in) at.row = (uint32_t)id * p.s_page + ((uint32_t)pos - page * p.page.d) * p.s_token;
         }
-        before += (int64_t)r.tiles * heads;
+        at.valid = (uint32_t)__ballot(in);
+        return at;
+    };
+    Spots next = rows_at(t0 + wave);
+    S s;
+    s.begin((const T*)p.q + b * p.sq_b + (head + min(l, columns - 1)) * p.sq_h, l < columns, u, p.D);
+    if constexpr (AHEAD) {
+        // Two tiles in turn, one loaded while the other is worked in (a copy
+        // from one to the other would wait for the loads).  What lies past t1 is
+        // nothing, and adds nothing.
+        typename S::Tile one, two;
+        S::load(one, kb, vb, next, l, u, p.D);
+        next = rows_at(t0 + wave + WAVES);
+        for (int t = t0 + wave; t < t1; t += 2 * WAVES) {
+            S::load(two, kb, vb, next, l, u, p.D);
+            next = rows_at(t + 2 * WAVES);
+            s.use(one, u, p.scale_log2);
+            S::load(one, kb, vb, next, l, u, p.D);
+            next = rows_at(t + 3 * WAVES);
+            s.use(two, u, p.scale_log2);
+        }
+    } else {
+        for (int t = t0 + wave; t < t1; t += WAVES) {
+            typename S::Tile now;
+            S::load(now, kb, vb, next, l, u, p.D);
+            next = rows_at(t + WAVES);
+            s.use(now, u, p.scale_log2);
+        }
+    }
+    s.run.sum += __shfl_xor(s.run.sum, 16);
+    s.run.sum += __shfl_xor(s.run.sum, 32);
+    __syncthreads();   // (the last row's parts have been read)
+    if (u == 0) { join.m[wave][l] = s.run.m; join.sum[wave][l] = s.run.sum; }
+#pragma unroll
+    for (int j = 0; j < CH; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) join.acc[wave][(4 * u + i) * CH + j][l] = s.acc[j][i];
+    __syncthreads();
+    for (int e = threadIdx.x; e < columns * DP; e += WAVES * 64) {
+        const int g = e / DP, c = e % DP;
+        float m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, join.m[w][g]);
+        const float base = m == -INFINITY ? 0.0f : m;
+        float y = 0.0f, sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float a = __builtin_amdgcn_exp2f(join.m[w][g] - base);
+            y += join.acc[w][c][g] * a;
+            sum += join.sum[w][g] * a;
+        }
+        if (whole) {
+            finish<T>(p, b, head + g, c, m, y, sum);
+        } else {
+            part[g * (DP + 2) + c] = y;
+            if (c == 0) { part[g * (DP + 2) + DP] = m; part[g * (DP + 2) + DP + 1] = sum; }
+        }
     }
 }
 
-// Rows that were cut between workgroups: their parts, in order.  Rows without
-// tokens: zeros.  A block takes a row (request, key head, head tile).
-template <class E, int DP>
-__global__ __launch_bounds__(256) void swr_paged_join_kernel(PagedParams p) {
-    typedef typename E::T T;
-    __shared__ int64_t buf[8];
+// Rows without a token: zeros.
+template <class T>
+__device__ inline void nothing(const PagedParams& p, int b, int64_t head, int columns) {
+    for (int e = threadIdx.x; e < columns * p.D; e += blockDim.x)
+        finish<T>(p, b, head + e / p.D, e % p.D, 0.0f, 0.0f, 0.0f);
+}
+
+// Waves of the kernel below that a SIMD holds (a compute unit as many blocks).
+constexpr int waves_held(int head_bytes) { return head_bytes <= 256 ? 3 : 1; }
+
+template <class E, int DP, bool FULL>
+__global__ __launch_bounds__(kWaves * 64, waves_held(DP * sizeof(typename E::T))) void swr_paged_kernel(PagedParams p) {
+    __shared__ int64_t buf[6];
+    __shared__ Joined<E, DP, kWaves> join;
+    const int heads = p.kv_heads * p.head_tiles;
+    for (int b = blockIdx.x; b < p.batch; b += gridDim.x)
+        if (rows_of(p, b).tiles == 0) nothing<typename E::T>(p, b, 0, p.kv_heads * p.group);
+    const Place f = find(p, heads, buf);
+    const int64_t begin = blockIdx.x * f.per, end = min(begin + f.per, f.total);
+    int4 cut = make_int4(0, 0, 0, 0);   // the row that begins here and goes on in the next shares
+    int64_t at = begin, before = f.before;
+    for (int b = f.b; at < end; ++b) {
+        const Rows r = rows_of(p, b);
+        if (r.tiles == 0) continue;
+        const int length = r.tiles + kRowCost;
+        for (int h = (int)((at - before) / length); h < heads && at < end; ++h) {
+            const int64_t tile0 = before + (int64_t)h * length + kRowCost;   // the place of the row's first tile
+            const int t0 = (int)max(at - tile0, (int64_t)0), t1 = (int)min((int64_t)r.tiles, end - tile0);
+            if (t0 < t1) {
+                // Parts: slot 0 of a row that began in an earlier share, slot 1 of one that goes on.
+                attend<E, DP, FULL, kWaves, false>(p, r, b, h, t0, t1, t0 == 0 && t1 == r.tiles,
+                                             p.part + (blockIdx.x * 2 + (t0 == 0 ? 1 : 0)) * part_floats(DP), join);
+                if (t0 == 0 && t1 < r.tiles)
+                    cut = make_int4(b, h, (int)((tile0 + r.tiles - 1) / f.per) - (int)blockIdx.x + 1, 0);
+            }
+            at = tile0 + t1;
+        }
+        before += places(r, heads);
+    }
+    if (threadIdx.x == 0) ((int4*)p.cuts)[blockIdx.x] = cut;
+}
+
+// Rows of few tokens, each a block's of its own: no shares to find or to join.
+// Eight waves, or four of wide heads, for their registers.
+constexpr int short_waves(size_t head_bytes) { return head_bytes >= 512 ? 4 : 8; }
+
+template <class E, int DP, bool FULL>
+__global__ __launch_bounds__(short_waves(DP * sizeof(typename E::T)) * 64) void swr_paged_short_kernel(PagedParams p) {
+    constexpr int WAVES = short_waves(DP * sizeof(typename E::T));
+    __shared__ Joined<E, DP, WAVES> join;
     const int heads = p.kv_heads * p.head_tiles;
     const int b = (int)(blockIdx.x / heads), h = (int)(blockIdx.x % heads);
-    // Tiles of all requests, and of those before b.
-    int64_t all = 0, prior = 0;
-    for (int i = threadIdx.x; i < p.batch; i += 256) {
-        const int n = rows_of(p, i).tiles;
-        all += n;
-        if (i < b) prior += n;
-    }
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) {
-        all += __shfl_xor(all, m);
-        prior += __shfl_xor(prior, m);
-    }
-    if (threadIdx.x % 64 == 0) { buf[threadIdx.x / 64 * 2] = all; buf[threadIdx.x / 64 * 2 + 1] = prior; }
-    __syncthreads();
-    const int64_t total = (buf[0] + buf[2] + buf[4] + buf[6]) * heads;
-    const int64_t per = max((total + p.workgroups - 1) / p.workgroups, (int64_t)kWaves);
     const Rows r = rows_of(p, b);
-    const int64_t row0 = (buf[1] + buf[3] + buf[5] + buf[7]) * heads + (int64_t)h * r.tiles;
-    const int64_t w0 = row0 / per, w1 = r.tiles ? (row0 + r.tiles - 1) / per : w0 - 1;
-    if (w0 == w1) return;
+    if (r.tiles == 0) {
+        const int g0 = h % p.head_tiles * 16;
+        nothing<typename E::T>(p, b, (int64_t)(h / p.head_tiles) * p.group + g0, min(p.group - g0, 16));
+        return;
+    }
+    attend<E, DP, FULL, WAVES, DP * sizeof(typename E::T) <= 256>(p, r, b, h, 0, r.tiles, true, nullptr, join);
+}
+
+// The row that begins in a workgroup's share and goes on past it, if there is
+// one (cuts): its parts there and in the workgroups after it.  The block's teams
+// of 128 threads take a channel of a column each and their share of the parts, 8 at a
+// time, and are joined in LDS, all in a fixed order.
+struct Sum {
+    float m = -INFINITY, y = 0.0f, sum = 0.0f;
+    __device__ void add(float pm, float py, float psum) {
+        const float top = fmaxf(m, pm), base = top == -INFINITY ? 0.0f : top;
+        const float a = __builtin_amdgcn_exp2f(m - base), z = __builtin_amdgcn_exp2f(pm - base);
+        y = y * a + py * z;
+        sum = sum * a + psum * z;
+        m = top;
+    }
+};
+
+__host__ __device__ inline bool by_row(int rows, int shares) { return rows < shares / 4; }
+
+template <class E, int DP>
+__global__ __launch_bounds__(1024) void swr_paged_join_kernel(PagedParams p) {
+    typedef typename E::T T;
+    __shared__ float buf[7][3][128];
+    // blockIdx.x is the share, or, where rows are few, the row (many blocks can
+    // then have a slice of it each, and few of them find nothing).
+    const int heads = p.kv_heads * p.head_tiles, rows = p.batch * heads;
+    int share = blockIdx.x;
+    if (by_row(rows, p.workgroups)) {
+        __shared__ int found;
+        if (threadIdx.x == 0) found = -1;
+        __syncthreads();
+        for (int i = threadIdx.x; i < p.workgroups; i += blockDim.x) {
+            const int4 c = ((const int4*)p.cuts)[i];
+            if (c.z > 0 && c.x * heads + c.y == (int)blockIdx.x) found = i;
+        }
+        __syncthreads();
+        share = found;
+        if (share < 0) return;
+    }
+    const int4 cut = ((const int4*)p.cuts)[share];
+    const int b = cut.x, h = cut.y, parts = cut.z;
+    if (parts == 0) return;
+    const int lane = threadIdx.x % 128, team = threadIdx.x / 128, teams = blockDim.x / 128;
     const int kv = h / p.head_tiles, g0 = h % p.head_tiles * 16, columns = min(p.group - g0, 16);
     const int64_t head = (int64_t)kv * p.group + g0;
-    // The first part is the first of its workgroup if the row starts that workgroup's share.
-    const int64_t first = w0 * 2 + (row0 > w0 * per ? 1 : 0);
-    for (int e = threadIdx.x; e < columns * DP; e += 256) {
-        const int g = e / DP, c = e % DP;
-        float m = -INFINITY, y = 0.0f, sum = 0.0f;
-        for (int64_t w = w0; w <= w1; ++w) {
-            const float* part = p.part + (w == w0 ? first : 2 * w) * part_floats(DP) + g * (DP + 2);
-            const float pm = part[DP], top = fmaxf(m, pm), base = top == -INFINITY ? 0.0f : top;
-            const float a = exp2f(m - base), z = exp2f(pm - base);
-            y = y * a + part[c] * z;
-            sum = sum * a + part[DP + 1] * z;
-            m = top;
+    // Part w is slot 1 of this share, then slot 0 of the next ones.
+    const float* base = p.part + (int64_t)share * 2 * part_floats(DP);
+    for (int e0 = blockIdx.y * 128; e0 < columns * DP; e0 += gridDim.y * 128) {
+        const int e = e0 + lane, g = min(e / DP, columns - 1), c = e % DP;
+        Sum s;
+        for (int w0 = team; w0 < parts; w0 += 8 * teams) {
+            float m[8], y[8], sum[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int w = min(w0 + teams * k, parts - 1);
+                const float* part = base + (w == 0 ? 1 : 2 * (int64_t)w) * part_floats(DP) + g * (DP + 2);
+                m[k] = w0 + teams * k < parts ? part[DP] : -INFINITY;
+                sum[k] = part[DP + 1];
+                y[k] = part[c];
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (w0 + teams * k < parts) s.add(m[k], y[k], sum[k]);
         }
-        finish<T>(p, b, head + g, c, m, y, sum);
+        __syncthreads();   // (the last channels' sums have been read)
+        if (team > 0) { buf[team - 1][0][lane] = s.m; buf[team - 1][1][lane] = s.y; buf[team - 1][2][lane] = s.sum; }
+        __syncthreads();
+        if (team == 0 && e < columns * DP) {
+            for (int k = 0; k < teams - 1; ++k) s.add(buf[k][0][lane], buf[k][1][lane], buf[k][2][lane]);
+            finish<T>(p, b, head + g, c, s.m, s.y, s.sum);
+        }
     }
 }
 
 int padded(int64_t D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
-template <class E, int DP>
+template <class E, int DP, bool FULL>
 hipError_t go(const PagedParams& p, hipStream_t st) {
-    hipLaunchKernelGGL((swr_paged_kernel<E, DP>), dim3((unsigned)p.workgroups), dim3(kWaves * 64), 0, st, p);
+    if (p.workgroups == 0) {
+        hipLaunchKernelGGL((swr_paged_short_kernel<E, DP, FULL>), dim3((unsigned)(p.batch * p.kv_heads * p.head_tiles)),
+                           dim3(short_waves(DP * sizeof(typename E::T)) * 64), 0, st, p);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((swr_paged_kernel<E, DP, FULL>), dim3((unsigned)p.workgroups), dim3(kWaves * 64), 0, st, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((swr_paged_join_kernel<E, DP>), dim3((unsigned)(p.batch * p.kv_heads * p.head_tiles)), dim3(256),
-                       0, st, p);
+    // Two teams where a row has a few parts on average, up to eight where it has many.
+    const int rows = p.batch * p.kv_heads * p.head_tiles, shares = p.workgroups;
+    const int teams = rows >= shares / 8 ? 2 : rows >= shares / 64 ? 4 : 8;
+    const int slices = std::min((std::min(p.group, 16) * DP + 127) / 128, by_row(rows, shares) ? 32 : 4);
+    hipLaunchKernelGGL((swr_paged_join_kernel<E, DP>), dim3((unsigned)(by_row(rows, shares) ? rows : shares), (unsigned)slices),
+                       dim3(128 * teams), 0, st, p);
     return hipGetLastError();
+}
+
+template <class E, int DP>
+hipError_t by_fill(const PagedParams& p, hipStream_t st) {
+    return p.D == DP ? go<E, DP, true>(p, st) : go<E, DP, false>(p, st);
 }
 
 template <class E>
 hipError_t by_width(const PagedParams& p, hipStream_t st) {
     switch (padded(p.D)) {
-        case 32: return go<E, 32>(p, st);
-        case 64: return go<E, 64>(p, st);
-        case 128: return go<E, 128>(p, st);
-        default: return go<E, 256>(p, st);
+        case 32: return by_fill<E, 32>(p, st);
+        case 64: return by_fill<E, 64>(p, st);
+        case 128: return by_fill<E, 128>(p, st);
+        default: return by_fill<E, 256>(p, st);
     }
 }
 
 }  // namespace
 
 int paged_workgroups(const swr_paged_t& p) {
-    const int64_t positions = p.window > 0 ? std::min(p.window, p.max_pages * p.cache.page_size)
-                                           : p.max_pages * p.cache.page_size;
+    const int64_t table = p.max_pages * p.cache.page_size;
+    const int64_t positions = p.window > 0 ? std::min(p.window, table) : table;
+    if (positions <= kShort) return 0;
     const int64_t heads = p.cache.heads * ((p.q_heads / p.cache.heads + 15) / 16);
     const double tiles = (double)p.batch * (double)heads * (double)((positions + kTile - 1) / kTile);
-    return (int)std::max(1.0, std::min(1024.0, (tiles + kWaves - 1) / kWaves));
+    return (int)std::min((double)kShares, (tiles + kWaves - 1) / kWaves);
 }
 
-int64_t paged_part_floats(const swr_paged_t& p) { return part_floats(padded(p.cache.D)); }
+int64_t paged_work_floats(const swr_paged_t& p) {
+    return (int64_t)paged_workgroups(p) * (2 * part_floats(padded(p.cache.D)) + 4);
+}
 
 hipError_t launch_tables(const TableParams& p, void* stream) {
     const int64_t blocks = std::max<int64_t>(1, (p.tokens + kTableTokens - 1) / kTableTokens);

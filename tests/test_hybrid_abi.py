@@ -266,7 +266,7 @@ def test_append_refuses():
 def _paged(**kw):
     p = hybrid.SwrPaged()
     _cache_of(p)
-    p.batch, p.q_heads, p.max_pages, p.st, p.window, p.scale = 3, 8, 10, 10, 0, 0.125
+    p.batch, p.q_heads, p.max_pages, p.st, p.window, p.scale = 3, 8, 100, 100, 0, 0.125
     p.sq_b = p.sy_b = 8 * 64
     p.sq_h = p.sy_h = 64
     for k, x in kw.items():
@@ -302,6 +302,10 @@ def test_attention_refuses_pointers():
         for i in range(5):
             assert _attention(_paged(), **{out: i}) == E_ALIAS
     assert _attention(_paged(), lse=5) == _attention(_paged(), ws=5) == _attention(_paged(), ws=6) == E_ALIAS
+    # a table of few positions, or a short window, is attended to without a workspace
+    size = hybrid._lib().swr_paged_workspace_bytes
+    assert size(ctypes.byref(_paged())) > 0
+    assert size(ctypes.byref(_paged(max_pages=10, st=10))) == size(ctypes.byref(_paged(window=64))) == 0
     assert _attention(_paged(batch=0), None, None, None, None, None, None, None, None) == OK
 
 
