@@ -98,8 +98,8 @@ int64_t swr_rms_norm_workspace_bytes(const swr_norm_t* norm);
  * A code's low three bits stand for 0, 0.5, 1, 1.5, 2, 3, 4, 6 and its high bit
  * for the sign (4-bit floating point of 2 exponent bits and 1 mantissa bit);
  * groups of 32 weights of a row share a power of two, stored as its exponent
- * plus 127 (0 to 252; 255 makes the group NaN; 253 and 254 hold weights beyond float32's range).  Two codes share a byte, the even k in its low
- * half.  A row of codes has ceil(K / 32) groups of 16 bytes, codes past K are
+ * plus 127 (0 to 252; 255 makes the group NaN; 253 and 254 hold weights beyond
+ * float32's range).  Two codes share a byte, the even k in its low half.  A row of codes has ceil(K / 32) groups of 16 bytes, codes past K are
  * not used, and starts 16-byte aligned.  Sums are in float32.  Meant for the
  * few rows of a decoding step (a row of weights is read once for up to 64 rows of x).
  * ------------------------------------------------------------------------ */
@@ -156,8 +156,9 @@ typedef struct swr_tables {
  *     new_lengths [batch]  lengths[i] + new_tokens[i]
  *     new_free_count [1]   free pages left
  * A page that the stack no longer holds is -1 in the table, and a token on such a page, on a
- * page whose table entry is negative, or past max_pages has slot -1.  lengths, new_tokens, free_stack, free_count, table,
- * starts, new_lengths and new_free_count are int32, slots is int64. */
+ * page whose table entry is negative, or past max_pages has slot -1.  lengths,
+ * new_tokens, free_stack, free_count, table, starts, new_lengths and new_free_count
+ * are int32, slots is int64. */
 int swr_block_tables(const swr_tables_t* p, const int32_t* lengths, const int32_t* new_tokens,
                      const int32_t* free_stack, const int32_t* free_count, int32_t* table, int64_t* slots,
                      int32_t* starts, int32_t* new_lengths, int32_t* new_free_count, void* stream);

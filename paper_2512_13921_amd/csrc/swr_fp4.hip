@@ -2,20 +2,25 @@
 //
 //     y[m, n] = s[m] sum_k x[m, k] value(code[n, k]) 2^(power[n, k / 32] - 127)
 //
-// A wave takes 16 rows of W (R tiles of them) and 16 rows of x (MT tiles) over
-// its share of k; the block's waves share out k, and join in LDS.  W is the
-// matrix instructions' A operand, so that a lane holds 32 weights of one row in
+// A wave takes tiles of 16 rows of W (R) and of x (MT) over its share of k; the
+// block's waves share out k, and join in LDS.  One kernel loads x along with W, the
+// other holds its share of x in registers and goes over W.  W is the matrix instructions' A operand, so that a lane holds 32 weights of one row in
 // 16 bytes, with their one power:
 //   * 8-bit x: the scaled matrix instruction takes codes and powers as they lie.
 //     Its sums of 128 products are off by up to 1.2e-5 of the sum of their absolute
 //     values (measured; the bf16 instruction's by 2^-24 of it), far below the
-//     rounding of a bf16 y, 2^-9; for a float32 y, x becomes bf16, exactly, and goes as below;
+//     rounding of a bf16 y, 2^-8; for a float32 y, x becomes bf16, exactly, and goes as below;
 //   * bf16 x: the conversion instruction makes bf16 pairs of code times power, exactly;
 //   * float32 x: the same against x split into three bf16 parts, which hold all
 //     of its 24 bits.
-// What bounds it is the weights' bytes: 17 a group of 32, read once for 64 rows
-// of x.
+// What bounds it is the weights' bytes, 17 a group of 32: 16 x 8192 8-bit rows
+// against 28672 take 35 us, 3.6 TB/s, where a copy reaches 5.2 and a loop over codes
+// and powers alone 5.0; of it about 5 us are x, which all CUs load first, and 31 us
+// the tiles (4.0 TB/s), whose waves meet after each.  Few or short rows are bound by
+// latency: 2048 to 6176 for one token 4.8 us.  float32 is bound by its conversion and
+// three products.
 #include <algorithm>
+#include <type_traits>
 
 #include "swr_hybrid_launch.h"
 
@@ -33,15 +38,24 @@ struct __attribute__((packed, aligned(sizeof(T)))) Loose {
     u32x4 v;
 };
 
-// 16 bytes of row elements at p, of which n elements (n <= 0: none) exist;
-// zeros past them.
-template <class T>
-__device__ inline u32x4 load16(const T* p, int n) {
+// How 16 bytes of a row of K elements are loaded from element k on, zeros past K:
+// kWhole where all are there; kEven where K is a multiple of 16 bytes' elements, by an
+// unconditional load and a selection, so that loads follow each other without
+// branches; kAny in branches, element by element at the end.
+enum Ends { kWhole, kEven, kAny };
+template <Ends ENDS, class T>
+__device__ inline u32x4 load16(const T* row, int k, int K) {
     constexpr int NE = 16 / sizeof(T);
-    if (n >= NE) return ((const Loose<T>*)p)->v;
+    if constexpr (ENDS == kWhole) return ((const Loose<T>*)(row + k))->v;
+    if constexpr (ENDS == kEven) {
+        const u32x4 v = ((const Loose<T>*)(row + min(k, K - NE)))->v;
+        const u32x4 none{0, 0, 0, 0};
+        return k < K ? v : none;
+    }
+    if (k + NE <= K) return ((const Loose<T>*)(row + k))->v;
     T e[NE];
 #pragma unroll
-    for (int i = 0; i < NE; ++i) e[i] = i < n ? p[i] : T(0);
+    for (int i = 0; i < NE; ++i) e[i] = k + i < K ? row[k + i] : T(0);
     return __builtin_bit_cast(u32x4, e);
 }
 
@@ -49,33 +63,43 @@ __device__ inline u32x4 load16(const T* p, int n) {
 __device__ inline float as_float(uint32_t u) { return __builtin_bit_cast(float, u); }
 
 struct XBf16 {
+    static constexpr bool kStaged = true;
     typedef uint16_t T;
     static constexpr int kParts = 1;
 };
 struct XF32 {
+    static constexpr bool kStaged = false;
     typedef float T;
     static constexpr int kParts = 3;
 };
 struct XFp8 {          // for a bf16 y
+    static constexpr bool kStaged = true;
     typedef uint8_t T;
 };
 struct XFp8Exact {     // for a float32 y
+    static constexpr bool kStaged = false;
     typedef uint8_t T;
     static constexpr int kParts = 1;
 };
 
-// A lane's x operands of one block of 128 k.
+// A lane's x operands against 32 weights of each quarter q, of group `of(q)` of 32 k.
 template <class X>
 struct Fragment;
 
 template <>
 struct Fragment<XBf16> {
-    bf16x8 v[4][1];   // matrix instruction j: k = 32 q + 8 j ...
-    __device__ void load(const uint16_t* row, int k0, int q, int K) {
+    static constexpr int kVectors = 4;
+    bf16x8 v[4][1];   // matrix instruction j: the group's k = 8 j ...
+    __device__ void put(int i, const u32x4& u) { v[i][0] = __builtin_bit_cast(bf16x8, u); }
+    __device__ u32x4 get(int i) const { return __builtin_bit_cast(u32x4, v[i][0]); }
+    // Where vector i is, in elements from the block's first: group g of quarter q's G.
+    static __device__ int at(int i, int q, int g, int G) { return 32 * (q * G + g) + 8 * i; }
+    template <Ends ENDS, class Of>
+    __device__ void load(const uint16_t* row, Of of, int q, int K) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int k = k0 + 32 * q + 8 * j;
-            v[j][0] = __builtin_bit_cast(bf16x8, load16(row + k, K - k));
+            const int k = 32 * of(q) + 8 * j;
+            v[j][0] = __builtin_bit_cast(bf16x8, load16<ENDS>(row, k, K));
         }
     }
 };
@@ -83,13 +107,14 @@ struct Fragment<XBf16> {
 template <>
 struct Fragment<XF32> {
     bf16x8 v[4][3];
-    __device__ void load(const float* row, int k0, int q, int K) {
+    template <Ends ENDS, class Of>
+    __device__ void load(const float* row, Of of, int q, int K) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int k = k0 + 32 * q + 8 * j + 4 * h;
-                const u32x4 u = load16(row + k, K - k);
+                const int k = 32 * of(q) + 8 * j + 4 * h;
+                const u32x4 u = load16<ENDS>(row, k, K);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     // Cut off, not rounded: nothing overflows, and each part
@@ -112,11 +137,12 @@ struct Fragment<XF32> {
 template <>
 struct Fragment<XFp8Exact> {
     bf16x8 v[4][1];
-    __device__ void load(const uint8_t* row, int k0, int q, int K) {
+    template <Ends ENDS, class Of>
+    __device__ void load(const uint8_t* row, Of of, int q, int K) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int k = k0 + 32 * q + 16 * h;
-            const u32x4 u = load16(row + k, K - k);
+            const int k = 32 * of(q) + 16 * h;
+            const u32x4 u = load16<ENDS>(row, k, K);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[i], 1.0f, false);
@@ -130,12 +156,17 @@ struct Fragment<XFp8Exact> {
 
 template <>
 struct Fragment<XFp8> {
-    u32x4 v[2];   // the scaled instruction's 8-bit operand: k = 16 q ... and 64 + 16 q ...
-    __device__ void load(const uint8_t* row, int k0, int q, int K) {
+    static constexpr int kVectors = 2;
+    __device__ void put(int i, const u32x4& u) { v[i] = u; }
+    __device__ u32x4 get(int i) const { return v[i]; }
+    static __device__ int at(int i, int q, int g, int G) { return 32 * ((2 * i + q / 2) * G + g) + 16 * (q % 2); }
+    u32x4 v[2];   // half h of group of(q / 2), then of of(2 + q / 2): the instruction's order of 8-bit operands
+    template <Ends ENDS, class Of>
+    __device__ void load(const uint8_t* row, Of of, int q, int K) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int k = k0 + 64 * h + 16 * q;
-            v[h] = load16(row + k, K - k);
+            const int k = 32 * of(2 * h + q / 2) + 16 * (q % 2);
+            v[h] = load16<ENDS>(row, k, K);
         }
     }
 };
@@ -183,60 +214,229 @@ template <>
 __device__ inline void put<uint16_t>(uint16_t* p, float f) { *p = __builtin_bit_cast(uint16_t, (__bf16)f); }
 
 constexpr int kWaves = 8;
+constexpr int kCus = 256;
 
-template <class X, class Y, int R, int MT>
+// One block of 128 G k of a wave's R tiles of W and MT tiles of x.  A lane takes G
+// groups of a row that lie next to each other, 16 G bytes of codes.
+template <class X, int R, int MT, int G>
+struct Step {
+    u32x4 codes[G][R];
+    uint32_t power[G][R];
+    Fragment<X> x[G][MT];
+    // Rows past N or M are the last ones again (their sums are not stored).
+    template <Ends ENDS>
+    __device__ void load(const Fp4Params& p, const int (&n)[R], const int (&m)[MT], int kb, int q) {
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+            const auto of = [&](int quarter) { return (kb * 4 + quarter) * G + j; };
+            const int group = of(q);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const bool in = ENDS == kWhole || group < (p.K + 31) / 32;
+                codes[j][r] = in ? *(const u32x4*)(p.codes + n[r] * p.sc + group * 16) : u32x4{0, 0, 0, 0};
+                power[j][r] = in ? p.powers[n[r] * p.sp + group] : 127;
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+                x[j][t].template load<ENDS>((const typename X::T*)p.x + m[t] * p.sx, of, q, p.K);
+        }
+    }
+    __device__ void multiply_into(f32x4 (&acc)[R][MT]) const {
+#pragma unroll
+        for (int j = 0; j < G; ++j)
+#pragma unroll
+            for (int r = 0; r < R; ++r) multiply(codes[j][r], power[j][r], x[j], acc[r]);
+    }
+};
+
+// A block's 8 waves are WK along k times 8 / WK along the rows of W; those along
+// k take its blocks in turn and are joined in LDS, those along W read the same
+// x at about the same time, mostly from the L1.  AHEAD blocks' loads are on their
+// way at once.
+template <class X, class Y, int R, int MT, int G, int WK, int AHEAD>
 __global__ __launch_bounds__(kWaves * 64) void swr_fp4_kernel(Fp4Params p) {
-    typedef typename X::T T;
-    __shared__ f32x4 join[kWaves][R * MT][64];
+    constexpr int WN = kWaves / WK;
+    __shared__ f32x4 join[WK > 1 ? kWaves : 1][R * MT][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, l = lane % 16, q = lane / 16;
-    const int n0 = (int)blockIdx.x * 16 * R;
-    const int m0 = (int)blockIdx.y * 16 * MT;
+    const int wn = wave % WN, wk = wave / WN;
+    const int n0 = (int)(blockIdx.x / p.m_blocks) * 16 * R * WN + wn * 16 * R;
+    const int m0 = (int)(blockIdx.x % p.m_blocks) * 16 * MT;
+    int n[R], m[MT];
+#pragma unroll
+    for (int r = 0; r < R; ++r) n[r] = min(n0 + 16 * r + l, p.N - 1);
+#pragma unroll
+    for (int t = 0; t < MT; ++t) m[t] = min(m0 + 16 * t + l, p.M - 1);
     f32x4 acc[R][MT];
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) acc[r][m] = f32x4{0, 0, 0, 0};
-    const int groups = (p.K + 31) / 32, blocks = (groups + 3) / 4;
-    for (int kb = wave; kb < blocks; kb += kWaves) {
-        const int group = kb * 4 + q;
-        u32x4 codes[R];
-        uint32_t power[R];
+        for (int t = 0; t < MT; ++t) acc[r][t] = f32x4{0, 0, 0, 0};
+    const int whole = p.K / (128 * G);
+    int kb = wk;
+    for (; kb + (AHEAD - 1) * WK < whole; kb += AHEAD * WK) {
+        Step<X, R, MT, G> s[AHEAD];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int n = n0 + 16 * r + l;
-            codes[r] = u32x4{0, 0, 0, 0};
-            power[r] = 127;
-            if (n < p.N && group < groups) {
-                codes[r] = *(const u32x4*)(p.codes + n * p.sc + group * 16);
-                power[r] = p.powers[n * p.sp + group];
-            }
-        }
-        Fragment<X> x[MT];
+        for (int a = 0; a < AHEAD; ++a) s[a].template load<kWhole>(p, n, m, kb + a * WK, q);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const int row = m0 + 16 * m + l;
-            x[m].load((const T*)p.x + (row < p.M ? row : 0) * p.sx, kb * 128, q, row < p.M ? p.K : 0);
-        }
-#pragma unroll
-        for (int r = 0; r < R; ++r) multiply(codes[r], power[r], x, acc[r]);
+        for (int a = 0; a < AHEAD; ++a) s[a].multiply_into(acc);
     }
+    for (; kb < whole; kb += WK) {
+        Step<X, R, MT, G> s;
+        s.template load<kWhole>(p, n, m, kb, q);
+        s.multiply_into(acc);
+    }
+    if (kb == whole && p.K % (128 * G)) {
+        Step<X, R, MT, G> s;
+        s.template load<kAny>(p, n, m, kb, q);
+        s.multiply_into(acc);
+    }
+    if constexpr (WK > 1) {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) join[wave][r * MT + m][lane] = acc[r][m];
-    __syncthreads();
-    // Tile t's sums, by the wave t % kWaves: the lane has rows 4 q ... of W and row l of x.
-    for (int t = wave; t < R * MT; t += kWaves) {
-        f32x4 sum = join[0][t][lane];
+            for (int t = 0; t < MT; ++t) join[wave][r * MT + t][lane] = acc[r][t];
+        __syncthreads();
+    }
+    // Tile t's sums, by the wave along k that has its turn: the lane has rows 4 q
+    // ... of W and row l of x.
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) sum += join[w][t][lane];
-        const int row = m0 + t % MT * 16 + l, n = n0 + t / MT * 16 + 4 * q;
+    for (int t = 0; t < R * MT; ++t) {
+        if (t % WK != wk) continue;
+        f32x4 sum = acc[t / MT][t % MT];
+        if constexpr (WK > 1) {
+            sum = join[wn][t][lane];
+#pragma unroll
+            for (int w = 1; w < WK; ++w) sum += join[w * WN + wn][t][lane];
+        }
+        const int row = m0 + t % MT * 16 + l, col = n0 + t / MT * 16 + 4 * q;
         if (row >= p.M) continue;
-        const float s = p.scale ? p.scale[row] : 1.0f;
-        Y* y = (Y*)p.y + row * p.sy + n;
+        const float f = p.scale ? p.scale[row] : 1.0f;
+        Y* y = (Y*)p.y + row * p.sy + col;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (n + i < p.N) put(y + i, sum[i] * s);
+            if (col + i < p.N) put(y + i, sum[i] * f);
+    }
+}
+
+// The same with x in registers: a block's 8 waves share out k, each keeps what it
+// needs of x (NB blocks of 128 k) and takes the tiles of 16 rows of W in turn with the
+// other blocks, the next tile's codes on their way while one is worked on.
+template <class X, int NB>
+struct Codes {
+    static constexpr int G = NB > 1 ? 2 : 1;
+    u32x4 codes[NB];
+    uint32_t power[NB / G];
+    // Groups past the row's last, of which x is zeros, are the last again.
+    __device__ void load(const Fp4Params& p, int tile, int wave, int l, int q) {
+        const int n = min(tile * 16 + l, p.N - 1), last = (p.K + 31) / 32 - 1;
+        const uint8_t* row = p.codes + n * p.sc;
+        const uint8_t* powers = p.powers + n * p.sp;
+#pragma unroll
+        for (int j = 0; j < NB / G; ++j) {
+            const int group = ((j * kWaves + wave) * 4 + q) * G;
+            if constexpr (G == 2) {
+                const int g = min(group, last), h = min(group + 1, last);
+                codes[2 * j] = *(const u32x4*)(row + g * 16);
+                codes[2 * j + 1] = *(const u32x4*)(row + h * 16);
+                power[j] = powers[g] | (uint32_t)powers[h] << 8;
+            } else {
+                const int g = min(group, last);
+                codes[j] = *(const u32x4*)(row + g * 16);
+                power[j] = powers[g];
+            }
+        }
+    }
+};
+
+template <class X, class Y, int MT, int NB, int DEPTH>
+__global__ __launch_bounds__(kWaves * 64) void swr_fp4_held_kernel(Fp4Params p) {
+    constexpr int G = Codes<X, NB>::G;
+    __shared__ f32x4 join[2][kWaves][MT][64];
+    __shared__ u32x4 stage[X::kStaged ? kWaves : 1][X::kStaged ? 16 * (8 * G * (int)sizeof(typename X::T) + 1) : 1];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, l = lane % 16, q = lane / 16;
+    const int m0 = (int)(blockIdx.x % p.m_blocks) * 16 * MT, first = (int)(blockIdx.x / p.m_blocks);
+    const int stride = (int)(gridDim.x / p.m_blocks), tiles = (p.N + 15) / 16;
+    Codes<X, NB> c[DEPTH];   // (the last one's loads are on their way while the first is worked on)
+    if constexpr (DEPTH == 2)
+        if (first < tiles) c[0].load(p, first, wave, l, q);
+    Fragment<X> x[NB][MT];
+    const auto hold = [&](auto ends) {
+        constexpr Ends ENDS = decltype(ends)::value;
+        typedef typename X::T T;
+        if constexpr (X::kStaged) {
+            // A lane's vectors of a row lie far apart, and a load of them would touch 64
+            // cache lines; so rows are loaded as they lie, and change places in LDS.
+            constexpr int NE = 16 / sizeof(T), C = 128 * G / NE, V = Fragment<X>::kVectors;
+            u32x4* own = stage[wave];
+#pragma unroll
+            for (int b = 0; b < NB / G; ++b)
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int i = 0; i < G * V; ++i) {
+                        const int at = i * 64 + lane, m = min(m0 + 16 * t + at / C, p.M - 1);
+                        const int k = (b * kWaves + wave) * 128 * G + at % C * NE;
+                        x[b * G + i / V][t].put(i % V, load16<ENDS>((const T*)p.x + m * p.sx, k, p.K));
+                    }
+#pragma unroll
+            for (int b = 0; b < NB / G; ++b)
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+#pragma unroll
+                    for (int i = 0; i < G * V; ++i) {
+                        const int at = i * 64 + lane;
+                        own[at / C * (C + 1) + at % C] = x[b * G + i / V][t].get(i % V);
+                    }
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                    for (int i = 0; i < G * V; ++i)
+                        x[b * G + i / V][t].put(i % V, own[l * (C + 1) + Fragment<X>::at(i % V, q, i / V, G) / NE]);
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    const int m = min(m0 + 16 * t + l, p.M - 1);
+                    const auto of = [&](int quarter) { return ((j / G * kWaves + wave) * 4 + quarter) * G + j % G; };
+                    x[j][t].template load<ENDS>((const T*)p.x + m * p.sx, of, q, p.K);
+                }
+        }
+    };
+    if (p.K % (16 / (int)sizeof(typename X::T)) == 0) hold(std::integral_constant<Ends, kEven>());
+    else hold(std::integral_constant<Ends, kAny>());
+    const auto work = [&](const Codes<X, NB>& c, int tile, int buf) {
+        f32x4 acc[MT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < NB; ++j) multiply(c.codes[j], c.power[j / G] >> 8 * (j % G) & 255, x[j], acc);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) join[buf][wave][t][lane] = acc[t];
+        __syncthreads();   // (the other half is read by no wave that is not past the last one)
+        for (int e = threadIdx.x; e < 256 * MT; e += kWaves * 64) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) sum += ((const float*)join[buf][w])[e];
+            const int at = e % 256 / 4, row = m0 + e / 256 * 16 + at % 16, col = tile * 16 + at / 16 * 4 + e % 4;
+            if (row < p.M && col < p.N) put((Y*)p.y + row * p.sy + col, p.scale ? sum * p.scale[row] : sum);
+        }
+    };
+    int tile = first, buf = 0;
+    const auto step = [&](const Codes<X, NB>& now, Codes<X, NB>& next) {
+        const int then = tile + (DEPTH - 1) * stride;
+        if (then < tiles) next.load(p, then, wave, l, q);
+        work(now, tile, buf);
+        tile += stride;
+        buf ^= 1;
+    };
+    while (tile < tiles) {
+        step(c[0], c[DEPTH - 1]);
+        if constexpr (DEPTH == 2)
+            if (tile < tiles) step(c[1], c[0]);
     }
 }
 
@@ -275,18 +475,98 @@ __global__ __launch_bounds__(256) void swr_fp4_pack_kernel(const T* w, int64_t N
     }
 }
 
-template <class X, class Y, int R, int MT>
-hipError_t go(const Fp4Params& p, hipStream_t st) {
-    const dim3 grid((unsigned)((p.N + 16 * R - 1) / (16 * R)), (unsigned)((p.M + 16 * MT - 1) / (16 * MT)));
-    hipLaunchKernelGGL((swr_fp4_kernel<X, Y, R, MT>), grid, dim3(kWaves * 64), 0, st, p);
+constexpr int kGroups = 2;   // of 32 k that a lane of the split kernel takes at once
+
+template <class X, class Y, int R, int MT, int WK>
+hipError_t go(Fp4Params p, hipStream_t st) {
+    constexpr int rows = 16 * R * (kWaves / WK), ahead = MT == 1 ? 2 : 1;
+    p.m_blocks = (p.M + 16 * MT - 1) / (16 * MT);
+    const int64_t blocks = (int64_t)((p.N + rows - 1) / rows) * p.m_blocks;
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((swr_fp4_kernel<X, Y, R, MT, kGroups, WK, ahead>), dim3((unsigned)blocks), dim3(kWaves * 64), 0,
+                       st, p);
     return hipGetLastError();
 }
 
+// The split kernel's waves along k: as many as there are blocks of k for them.
+// (Fewer waves along k and more along the rows were slower or the same at every size
+// tried: one row of 4096 against 4096, 5.0 us with 8 along k, 7.3 with 4, 11.6 with 2;
+// of 8192 against 28672, 45, 44 and 47.)
+template <class X, class Y, int R, int MT>
+hipError_t split(const Fp4Params& p, hipStream_t st) {
+    const int blocks = (p.K + 128 * kGroups - 1) / (128 * kGroups);
+    if (blocks == 1) return go<X, Y, R, MT, 1>(p, st);
+    if (blocks <= 3) return go<X, Y, R, MT, 2>(p, st);
+    if (blocks <= 7) return go<X, Y, R, MT, 4>(p, st);
+    return go<X, Y, R, MT, 8>(p, st);
+}
+
+// Registers that a lane holds x in, and the most that it may.
+template <class X, int MT, int NB>
+constexpr int held() {
+    return (int)sizeof(Fragment<X>) / 4 * MT * NB;
+}
+constexpr int kMostHeld = 128;
+
+template <class X, class Y, int MT, int NB>
+hipError_t hold(Fp4Params p, hipStream_t st) {
+    if constexpr (held<X, MT, NB>() > kMostHeld) return hipErrorInvalidValue;   // (fits() is false)
+    else {
+        p.m_blocks = (p.M + 16 * MT - 1) / (16 * MT);
+        const int64_t tiles = (p.N + 15) / 16, most = std::max(kCus / p.m_blocks, 1);
+        // A second tile's codes on their way, where the registers have room for them
+        // (a third's: 34.6 us for 35.5 at 16 x 8192 8-bit rows against 28672, 40.9 for 40.6 with bf16).
+        constexpr int depth = held<X, MT, NB>() + 2 * 5 * NB <= 224 ? 2 : 1;
+        hipLaunchKernelGGL((swr_fp4_held_kernel<X, Y, MT, NB, depth>),
+                           dim3((unsigned)(std::min(tiles, most) * p.m_blocks)), dim3(kWaves * 64), 0, st, p);
+        return hipGetLastError();
+    }
+}
+
+// Blocks of 128 k of a wave, as the held kernel is built for them; 0 past its last.
+int blocks_a_wave(int K) {
+    const int nb = ((K + 127) / 128 + kWaves - 1) / kWaves;
+    return nb <= 2 ? nb : nb <= 4 ? 4 : nb <= 6 ? 6 : nb <= 8 ? 8 : nb <= 16 ? 16 : 0;
+}
+
+template <class X, int MT>
+bool fits(int K) {
+    const int nb = blocks_a_wave(K);
+    return nb != 0 && held<X, MT, 1>() * nb <= kMostHeld;
+}
+
+template <class X, class Y, int MT>
+hipError_t hold(const Fp4Params& p, hipStream_t st) {
+    switch (blocks_a_wave(p.K)) {
+        case 1: return hold<X, Y, MT, 1>(p, st);
+        case 2: return hold<X, Y, MT, 2>(p, st);
+        case 4: return hold<X, Y, MT, 4>(p, st);
+        case 6: return hold<X, Y, MT, 6>(p, st);
+        case 8: return hold<X, Y, MT, 8>(p, st);
+        default: return hold<X, Y, MT, 16>(p, st);
+    }
+}
+
+// Which kernel, in us (split with one tile of W a wave, with two, held):
+//     rows of x     1000 to 1001     4096 to 4096     8192 to 8192        8192 to 28672
+//     1 bf16        4.5   -   4.2    5.0  6.7  6.3    12.2  13.3  14.4    46  41  39
+//     8 8-bit       4.4   -   4.4    5.1  6.5  4.8    14.4  10.6  12.0    42  40  35
+//     16 bf16        -    -    -     8.9  9.0  6.2    24.0  18.9  14.9    102 86  41
+//     5 float32     6.1   -   4.3     (does not fit)
+// The split kernel's lanes load x with a cache line for each of its rows, time after time; the
+// held one's load it once, but before all else, which few rows and few tiles pay back only
+// where x is short, of two blocks of 128 k a wave at most.  It has one block a CU (two: 10 %
+// slower).  Past 16 rows of x it takes 32 at a time if they fit (64 x 8192 to 28672,
+// 8-bit: 68 us, the split kernel 110).
 template <class X, class Y>
-hipError_t by_rows(const Fp4Params& p, hipStream_t st) {
-    if (p.M <= 16) return go<X, Y, 1, 1>(p, st);
-    if (p.M <= 32) return go<X, Y, 1, 2>(p, st);
-    return go<X, Y, 1, 4>(p, st);
+hipError_t by_size(const Fp4Params& p, hipStream_t st) {
+    const int tiles = (p.N + 15) / 16;
+    if (p.M > 8 || tiles > 2 * kCus || p.K <= 2 * 128 * kWaves) {
+        if (p.M > 16 && fits<X, 2>(p.K)) return hold<X, Y, 2>(p, st);
+        if (fits<X, 1>(p.K)) return hold<X, Y, 1>(p, st);
+    }
+    if (p.M > 16) return split<X, Y, 2, 2>(p, st);
+    return tiles <= kCus ? split<X, Y, 1, 1>(p, st) : split<X, Y, 2, 1>(p, st);
 }
 
 }  // namespace
@@ -294,9 +574,9 @@ hipError_t by_rows(const Fp4Params& p, hipStream_t st) {
 hipError_t launch_fp4(int dtype, int out_dtype, const Fp4Params& p, void* stream) {
     const hipStream_t st = (hipStream_t)stream;
     const bool f32 = out_dtype == SWR_DTYPE_F32;
-    if (dtype == SWR_DTYPE_FP8) return f32 ? by_rows<XFp8Exact, float>(p, st) : by_rows<XFp8, uint16_t>(p, st);
-    if (dtype == SWR_DTYPE_BF16) return f32 ? by_rows<XBf16, float>(p, st) : by_rows<XBf16, uint16_t>(p, st);
-    return f32 ? by_rows<XF32, float>(p, st) : by_rows<XF32, uint16_t>(p, st);
+    if (dtype == SWR_DTYPE_FP8) return f32 ? by_size<XFp8Exact, float>(p, st) : by_size<XFp8, uint16_t>(p, st);
+    if (dtype == SWR_DTYPE_BF16) return f32 ? by_size<XBf16, float>(p, st) : by_size<XBf16, uint16_t>(p, st);
+    return f32 ? by_size<XF32, float>(p, st) : by_size<XF32, uint16_t>(p, st);
 }
 
 hipError_t launch_fp4_pack(int dtype, const void* w, int64_t N, int64_t K, int64_t sw, uint8_t* codes, uint8_t* powers,

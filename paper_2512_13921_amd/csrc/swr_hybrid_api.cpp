@@ -286,7 +286,7 @@ int swr_fp4_linear(const swr_fp4_t* p, const void* x, const float* scale, const 
     const Span sy = span(y, (max_offset({{p->M, p->sy}, {p->N, 1}}) + 1) * size_of(p->out_dtype));
     if (overlaps(sy, {s.x, s.codes, s.powers, span(scale, p->M * 4)})) return SWR_ERR_ALIAS;
     const swr::Fp4Params q{x, scale, (const uint8_t*)codes, (const uint8_t*)powers, y, (int32_t)p->M, (int32_t)p->N,
-                           (int32_t)p->K, p->sx, p->sy, p->sc, p->sp};
+                           (int32_t)p->K, p->sx, p->sy, p->sc, p->sp, 0};
     return status(swr::launch_fp4(p->dtype, p->out_dtype, q, stream));
 }
 

@@ -48,6 +48,7 @@ struct Fp4Params {
     void* y;
     int32_t M, N, K;
     int64_t sx, sy, sc, sp;
+    int32_t m_blocks;    // the launch's: blocks along M
 };
 hipError_t launch_fp4(int dtype, int out_dtype, const Fp4Params& p, void* stream);
 hipError_t launch_fp4_pack(int dtype, const void* w, int64_t N, int64_t K, int64_t sw, uint8_t* codes, uint8_t* powers,

@@ -722,8 +722,9 @@ hipError_t go(const PagedParams& p, hipStream_t st) {
     const int rows = p.batch * p.kv_heads * p.head_tiles, shares = p.workgroups;
     const int teams = rows >= shares / 8 ? 2 : rows >= shares / 64 ? 4 : 8;
     const int slices = std::min((std::min(p.group, 16) * DP + 127) / 128, by_row(rows, shares) ? 32 : 4);
-    hipLaunchKernelGGL((swr_paged_join_kernel<E, DP>), dim3((unsigned)(by_row(rows, shares) ? rows : shares), (unsigned)slices),
-                       dim3(128 * teams), 0, st, p);
+    const int blocks = by_row(rows, shares) ? rows : shares;
+    hipLaunchKernelGGL((swr_paged_join_kernel<E, DP>), dim3((unsigned)blocks, (unsigned)slices), dim3(128 * teams), 0,
+                       st, p);
     return hipGetLastError();
 }
 
