@@ -341,7 +341,7 @@ int swr_block_tables(const swr_tables_t* p, const int32_t* lengths, const int32_
     q.table = table; q.slots = slots; q.starts = starts; q.new_lengths = new_lengths; q.new_count = new_free_count;
     q.batch = (int32_t)p->batch; q.max_pages = (int32_t)p->max_pages; q.page_size = (int32_t)p->page_size;
     q.free_pages = (int32_t)p->free_pages;
-    q.st = p->st; q.tokens = p->tokens;
+    q.st = p->st; q.tokens = p->tokens; q.page = swr::Divisor(p->page_size);
     return status(swr::launch_tables(q, stream));
 }
 

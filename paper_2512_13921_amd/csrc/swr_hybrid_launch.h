@@ -77,6 +77,7 @@ struct TableParams {
     int32_t *starts, *new_lengths, *new_count;
     int32_t batch, max_pages, page_size, free_pages;
     int64_t st, tokens;
+    Divisor page;                        // by the page size
 };
 hipError_t launch_tables(const TableParams& p, void* stream);
 
