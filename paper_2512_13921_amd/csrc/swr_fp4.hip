@@ -14,11 +14,10 @@
 //   * float32 x: the same against x split into three bf16 parts, which hold all
 //     of its 24 bits.
 // What bounds it is the weights' bytes, 17 a group of 32: 16 x 8192 8-bit rows
-// against 28672 take 35 us, 3.6 TB/s, where a copy reaches 5.2 and a loop over codes
-// and powers alone 5.0; of it about 5 us are x, which all CUs load first, and 31 us
-// the tiles (4.0 TB/s), whose waves meet after each.  Few or short rows are bound by
-// latency: 2048 to 6176 for one token 4.8 us.  float32 is bound by its conversion and
-// three products.
+// against 28672 take 33 us, 3.8 TB/s, where a copy reaches 5.2 and a loop over codes
+// and powers alone 5.0; of it about 6 us are x, which all CUs load first, and 27 us
+// the tiles (4.6 TB/s).  Few or short rows are bound by latency: 2048 to 6176 for one
+// token 4.9 us.  float32 is bound by its conversion and three products.
 #include <algorithm>
 #include <type_traits>
 
@@ -350,8 +349,8 @@ struct Codes {
 
 template <class X, class Y, int MT, int NB, int DEPTH>
 __global__ __launch_bounds__(kWaves * 64) void swr_fp4_held_kernel(Fp4Params p) {
-    constexpr int G = Codes<X, NB>::G;
-    __shared__ f32x4 join[2][kWaves][MT][64];
+    constexpr int G = Codes<X, NB>::G, TURNS = 4 / MT;
+    __shared__ f32x4 join[2][TURNS][kWaves][MT][64];
     __shared__ u32x4 stage[X::kStaged ? kWaves : 1][X::kStaged ? 16 * (8 * G * (int)sizeof(typename X::T) + 1) : 1];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, l = lane % 16, q = lane / 16;
     const int m0 = (int)(blockIdx.x % p.m_blocks) * 16 * MT, first = (int)(blockIdx.x / p.m_blocks);
@@ -408,35 +407,38 @@ __global__ __launch_bounds__(kWaves * 64) void swr_fp4_held_kernel(Fp4Params p) 
     };
     if (p.K % (16 / (int)sizeof(typename X::T)) == 0) hold(std::integral_constant<Ends, kEven>());
     else hold(std::integral_constant<Ends, kAny>());
-    const auto work = [&](const Codes<X, NB>& c, int tile, int buf) {
+    // A tile's sums of this wave.  The waves meet every TURNS tiles only, so that one may be
+    // ahead of another (16 x 8192 to 114688, 8-bit: 128 us with one, 120 with two, 115 with
+    // four; of bf16 141, 128, 121).
+    const auto work = [&](const Codes<X, NB>& c, int turn, int buf) {
         f32x4 acc[MT];
 #pragma unroll
         for (int t = 0; t < MT; ++t) acc[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < NB; ++j) multiply(c.codes[j], c.power[j / G] >> 8 * (j % G) & 255, x[j], acc);
 #pragma unroll
-        for (int t = 0; t < MT; ++t) join[buf][wave][t][lane] = acc[t];
-        __syncthreads();   // (the other half is read by no wave that is not past the last one)
-        for (int e = threadIdx.x; e < 256 * MT; e += kWaves * 64) {
+        for (int t = 0; t < MT; ++t) join[buf][turn][wave][t][lane] = acc[t];
+    };
+    for (int tile = first, buf = 0; tile < tiles; tile += TURNS * stride, buf ^= 1) {
+        int turns = 0;
+#pragma unroll
+        for (int h = 0; h < TURNS; ++h) {
+            const int now = tile + h * stride, then = now + (DEPTH - 1) * stride;
+            if (now >= tiles) break;
+            if (then < tiles) c[(h + DEPTH - 1) % DEPTH].load(p, then, wave, l, q);
+            work(c[h % DEPTH], h, buf);
+            ++turns;
+        }
+        __syncthreads();   // (the other buffer is read by no wave that is not past the last one)
+        for (int e = threadIdx.x; e < turns * 256 * MT; e += kWaves * 64) {
+            const int turn = e / (256 * MT), in = e % (256 * MT);
             float sum = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) sum += ((const float*)join[buf][w])[e];
-            const int at = e % 256 / 4, row = m0 + e / 256 * 16 + at % 16, col = tile * 16 + at / 16 * 4 + e % 4;
+            for (int w = 0; w < kWaves; ++w) sum += ((const float*)join[buf][turn][w])[in];
+            const int at = in % 256 / 4, row = m0 + in / 256 * 16 + at % 16;
+            const int col = (tile + turn * stride) * 16 + at / 16 * 4 + in % 4;
             if (row < p.M && col < p.N) put((Y*)p.y + row * p.sy + col, p.scale ? sum * p.scale[row] : sum);
         }
-    };
-    int tile = first, buf = 0;
-    const auto step = [&](const Codes<X, NB>& now, Codes<X, NB>& next) {
-        const int then = tile + (DEPTH - 1) * stride;
-        if (then < tiles) next.load(p, then, wave, l, q);
-        work(now, tile, buf);
-        tile += stride;
-        buf ^= 1;
-    };
-    while (tile < tiles) {
-        step(c[0], c[DEPTH - 1]);
-        if constexpr (DEPTH == 2)
-            if (tile < tiles) step(c[1], c[0]);
     }
 }
 
@@ -515,7 +517,7 @@ hipError_t hold(Fp4Params p, hipStream_t st) {
         p.m_blocks = (p.M + 16 * MT - 1) / (16 * MT);
         const int64_t tiles = (p.N + 15) / 16, most = std::max(kCus / p.m_blocks, 1);
         // A second tile's codes on their way, where the registers have room for them
-        // (a third's: 34.6 us for 35.5 at 16 x 8192 8-bit rows against 28672, 40.9 for 40.6 with bf16).
+        // (a third's gained 2 % at 16 x 8192 8-bit rows against 28672 and lost 1 % with bf16).
         constexpr int depth = held<X, MT, NB>() + 2 * 5 * NB <= 224 ? 2 : 1;
         hipLaunchKernelGGL((swr_fp4_held_kernel<X, Y, MT, NB, depth>),
                            dim3((unsigned)(std::min(tiles, most) * p.m_blocks)), dim3(kWaves * 64), 0, st, p);
@@ -549,15 +551,15 @@ hipError_t hold(const Fp4Params& p, hipStream_t st) {
 
 // Which kernel, in us (split with one tile of W a wave, with two, held):
 //     rows of x     1000 to 1001     4096 to 4096     8192 to 8192        8192 to 28672
-//     1 bf16        4.5   -   4.2    5.0  6.7  6.3    12.2  13.3  14.4    46  41  39
-//     8 8-bit       4.4   -   4.4    5.1  6.5  4.8    14.4  10.6  12.0    42  40  35
-//     16 bf16        -    -    -     8.9  9.0  6.2    24.0  18.9  14.9    102 86  41
+//     1 bf16        4.5   -   4.2    5.0  6.7  6.3    12.2  13.3  14.4    46  41  36
+//     8 8-bit       4.4   -   4.4    5.1  6.5  4.8    14.4  10.6  11.7    42  40  33
+//     16 bf16        -    -    -     8.9  9.0  6.3    24.0  18.9  14.3    102 86  37
 //     5 float32     6.1   -   4.3     (does not fit)
 // The split kernel's lanes load x with a cache line for each of its rows, time after time; the
 // held one's load it once, but before all else, which few rows and few tiles pay back only
 // where x is short, of two blocks of 128 k a wave at most.  It has one block a CU (two: 10 %
 // slower).  Past 16 rows of x it takes 32 at a time if they fit (64 x 8192 to 28672,
-// 8-bit: 68 us, the split kernel 110).
+// 8-bit: 65 us, the split kernel 110).
 template <class X, class Y>
 hipError_t by_size(const Fp4Params& p, hipStream_t st) {
     const int tiles = (p.N + 15) / 16;
