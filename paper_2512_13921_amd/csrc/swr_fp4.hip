@@ -4,8 +4,9 @@
 //
 // A wave takes tiles of 16 rows of W (R) and of x (MT) over its share of k; the
 // block's waves share out k, and join in LDS.  One kernel loads x along with W, the
-// other holds its share of x in registers and goes over W.  W is the matrix instructions' A operand, so that a lane holds 32 weights of one row in
-// 16 bytes, with their one power:
+// other holds its share of x in registers and goes over W.  W is the matrix
+// instructions' A operand, so that a lane holds 32 weights of one row in 16 bytes, with
+// their one power:
 //   * 8-bit x: the scaled matrix instruction takes codes and powers as they lie.
 //     Its sums of 128 products are off by up to 1.2e-5 of the sum of their absolute
 //     values (measured; the bf16 instruction's by 2^-24 of it), far below the

@@ -53,7 +53,8 @@ __device__ inline int64_t over(const TableParams& p, int64_t n) {
 
 // Every block sums the requests' new tokens and pages itself, 256 requests at
 // a time (sums of a launch before it would cost that launch, and the lengths are
-// a few KB in the L2), and writes its range of the slots and every
+// a few KB in the L2; 8 requests of one token 3.1 us, 200 of 1311 6.0, all of it
+// the chain of lengths, sums, search, page and slot), and writes its range of the slots and every
 // gridDim.x-th 256 of the new pages' entries.  The entries that it reads, of pages
 // that a request held before, are none that a block writes.
 __global__ __launch_bounds__(256) void swr_tables_kernel(TableParams p) {
@@ -118,7 +119,8 @@ __global__ __launch_bounds__(256) void swr_tables_kernel(TableParams p) {
 // Append
 // ---------------------------------------------------------------------------
 
-// A copy of 16-byte vectors; keys in the grid's first half of y, values in the second.
+// Bound by its bytes: 50021 tokens of 8 heads of 128, bf16, 73 us, 5.6 TB/s; 256
+// tokens 2.9 us, a launch.  A copy of 16-byte vectors; keys in the grid's first half of y, values in the second.
 __global__ __launch_bounds__(256) void swr_append_kernel(AppendParams p) {
     const bool values = blockIdx.y != 0;
     const u32x4* in = (const u32x4*)(values ? p.v : p.k);
@@ -156,10 +158,18 @@ __global__ __launch_bounds__(256) void swr_append_kernel(AppendParams p) {
 // workgroups, and no host knows the lengths.  Waves take a row's tiles in turn
 // and are joined in LDS.  A row cut between workgroups leaves its parts
 // in the workspace, which swr_paged_join_kernel joins.
+//
+// What bounds it is K and V, read once: 2 requests of 262147 tokens (4 heads of 128 for
+// 32, bf16) 378 to 390 us, 5.5 to 5.7 TB/s, where a copy reaches 5.2; 64 of 17 to 32768 tokens
+// 229 us, 4.9 TB/s, of which 5 are the join.  Short rows are bound by the trips to memory,
+// length, table, K, V: 4 requests of 300 to 700 tokens 11 us.
 
 constexpr int kTile = 32;      // tokens of a wave's tile
 constexpr int kWaves = 4;
-constexpr int kShort = 1024;   // positions up to which a row is one block's
+// Positions up to which a row is one block's.  (16 rows of 500 tokens, heads of 128, bf16:
+// 9.4 us, 13.2 in shares; of 1000 15.1 and 13.5, of 1500 20.3 and 14.0.  256 rows gain past it
+// if they are alike, 1500 tokens 42 and 50, and lose if not, 17 to 2000 tokens 27.6 and 23.3.)
+constexpr int kShort = 1024;
 // Shares of the work: three workgroups a compute unit, which is what a unit
 // holds of heads of up to 256 bytes.  Not a power of two: of equal rows, whose
 // lengths mostly are, shares would begin at multiples of large powers of two and so
@@ -183,7 +193,8 @@ __device__ inline Rows rows_of(const PagedParams& p, int b) {
 // The flat order: (request, head row within the request, place within the row).
 // A row takes kRowCost places, in which nothing is done, before its tiles: what
 // beginning and joining a row costs, in tiles, so that shares of many short rows are
-// no longer than others.
+// no longer than others (100 requests of 10 to 5000 tokens, 4 rows each: 45.0 us, with
+// 0 places 59.6).
 struct Place {
     int64_t total;   // places of all rows
     int64_t per;     // places a workgroup
@@ -627,12 +638,14 @@ __global__ __launch_bounds__(kWaves * 64, waves_held(DP * sizeof(typename E::T))
 }
 
 // Rows of few tokens, each a block's of its own: no shares to find or to join.
-// Eight waves, or four of wide heads, for their registers.
-constexpr int short_waves(size_t head_bytes) { return head_bytes >= 512 ? 4 : 8; }
+// Eight waves, or four of heads past 128 channels, for their registers (256 rows of 900
+// tokens: 256 channels of float32 209 us with eight, 106 with four, of bf16 52.6 and
+// 49.7; 128 of float32 52.3 and 57.3).
+constexpr int short_waves(int channels) { return channels > 128 ? 4 : 8; }
 
 template <class E, int DP, bool FULL>
-__global__ __launch_bounds__(short_waves(DP * sizeof(typename E::T)) * 64) void swr_paged_short_kernel(PagedParams p) {
-    constexpr int WAVES = short_waves(DP * sizeof(typename E::T));
+__global__ __launch_bounds__(short_waves(DP) * 64) void swr_paged_short_kernel(PagedParams p) {
+    constexpr int WAVES = short_waves(DP);
     __shared__ Joined<E, DP, WAVES> join;
     const int heads = p.kv_heads * p.head_tiles;
     const int b = (int)(blockIdx.x / heads), h = (int)(blockIdx.x % heads);
@@ -660,6 +673,8 @@ struct Sum {
     }
 };
 
+// Few rows are found by a block each, many by the shares that they begin in (4 rows of
+// 100000 tokens: 54.9 us, by shares 57.9; 800 of 1100 to 3000: 169.0, by shares 163.5).
 __host__ __device__ inline bool by_row(int rows, int shares) { return rows < shares / 4; }
 
 template <class E, int DP>
@@ -723,13 +738,14 @@ template <class E, int DP, bool FULL>
 hipError_t go(const PagedParams& p, hipStream_t st) {
     if (p.workgroups == 0) {
         hipLaunchKernelGGL((swr_paged_short_kernel<E, DP, FULL>), dim3((unsigned)(p.batch * p.kv_heads * p.head_tiles)),
-                           dim3(short_waves(DP * sizeof(typename E::T)) * 64), 0, st, p);
+                           dim3(short_waves(DP) * 64), 0, st, p);
         return hipGetLastError();
     }
     hipLaunchKernelGGL((swr_paged_kernel<E, DP, FULL>), dim3((unsigned)p.workgroups), dim3(kWaves * 64), 0, st, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    // Two teams where a row has a few parts on average, up to eight where it has many.
+    // Two teams where a row has a few parts on average, up to eight where it has many (800
+    // rows of 1100 to 3000 tokens 163.5 us, with eight 173.7; 4 rows of 100000 54.9, with two 61.0).
     const int rows = p.batch * p.kv_heads * p.head_tiles, shares = p.workgroups;
     const int teams = rows >= shares / 8 ? 2 : rows >= shares / 64 ? 4 : 8;
     const int slices = std::min((std::min(p.group, 16) * DP + 127) / 128, by_row(rows, shares) ? 32 : 4);
