@@ -7,17 +7,17 @@
 // other holds its share of x in registers and goes over W.  W is the matrix
 // instructions' A operand, so that a lane holds 32 weights of one row in 16 bytes, with
 // their one power:
-//   * 8-bit x: the scaled matrix instruction takes codes and powers as they lie.
-//     Its sums of 128 products are off by up to 1.2e-5 of the sum of their absolute
-//     values (measured; the bf16 instruction's by 2^-24 of it), far below the
-//     rounding of a bf16 y, 2^-8; for a float32 y, x becomes bf16, exactly, and goes as below;
 //   * bf16 x: the conversion instruction makes bf16 pairs of code times power, exactly;
+//   * 8-bit x: the same against x made bf16, exactly.  (The matrix instruction that takes
+//     codes, powers and 8-bit values as they lie would save the conversions, 33 us for 35
+//     below, but its sums of 128 products are off by up to 1.2e-5 of the sum of their
+//     absolute values, which shows in a bf16 y where they cancel);
 //   * float32 x: the same against x split into three bf16 parts, which hold all
 //     of its 24 bits.
 // What bounds it is the weights' bytes, 17 a group of 32: 16 x 8192 8-bit rows
-// against 28672 take 33 us, 3.8 TB/s, where a copy reaches 5.2 and a loop over codes
-// and powers alone 5.0; of it about 6 us are x, which all CUs load first, and 27 us
-// the tiles (4.6 TB/s).  Few or short rows are bound by latency: 2048 to 6176 for one
+// against 28672 take 35 us, 3.6 TB/s, where a copy reaches 5.2 and a loop over codes
+// and powers alone 5.0; of it about 7 us are x, which all CUs load first, and 28 us
+// the tiles (4.4 TB/s).  Few or short rows are bound by latency: 2048 to 6176 for one
 // token 4.9 us.  float32 is bound by its conversion and three products.
 #include <algorithm>
 #include <type_traits>
@@ -28,7 +28,6 @@ namespace swr {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -72,12 +71,8 @@ struct XF32 {
     typedef float T;
     static constexpr int kParts = 3;
 };
-struct XFp8 {          // for a bf16 y
+struct XFp8 {
     static constexpr bool kStaged = true;
-    typedef uint8_t T;
-};
-struct XFp8Exact {     // for a float32 y
-    static constexpr bool kStaged = false;
     typedef uint8_t T;
     static constexpr int kParts = 1;
 };
@@ -92,6 +87,7 @@ struct Fragment<XBf16> {
     bf16x8 v[4][1];   // matrix instruction j: the group's k = 8 j ...
     __device__ void put(int i, const u32x4& u) { v[i][0] = __builtin_bit_cast(bf16x8, u); }
     __device__ u32x4 get(int i) const { return __builtin_bit_cast(u32x4, v[i][0]); }
+    __device__ bf16x8 part(int j, int) const { return v[j][0]; }
     // Where vector i is, in elements from the block's first: group g of quarter q's G.
     static __device__ int at(int i, int q, int g, int G) { return 32 * (q * G + g) + 8 * i; }
     template <Ends ENDS, class Of>
@@ -107,6 +103,7 @@ struct Fragment<XBf16> {
 template <>
 struct Fragment<XF32> {
     bf16x8 v[4][3];
+    __device__ bf16x8 part(int j, int c) const { return v[j][c]; }
     template <Ends ENDS, class Of>
     __device__ void load(const float* row, Of of, int q, int K) {
 #pragma unroll
@@ -134,40 +131,30 @@ struct Fragment<XF32> {
     }
 };
 
-template <>
-struct Fragment<XFp8Exact> {
-    bf16x8 v[4][1];
-    template <Ends ENDS, class Of>
-    __device__ void load(const uint8_t* row, Of of, int q, int K) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int k = 32 * of(q) + 16 * h;
-            const u32x4 u = load16<ENDS>(row, k, K);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[i], 1.0f, false);
-                const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[i], 1.0f, true);
-                bf16x8& w = v[2 * h + i / 2][0];
-                w[i % 2 * 4] = a[0]; w[i % 2 * 4 + 1] = a[1]; w[i % 2 * 4 + 2] = b[0]; w[i % 2 * 4 + 3] = b[1];
-            }
-        }
-    }
-};
-
+// (Kept as they are, and made bf16, exactly, for each product: half the registers.)
 template <>
 struct Fragment<XFp8> {
     static constexpr int kVectors = 2;
+    u32x4 v[2];
     __device__ void put(int i, const u32x4& u) { v[i] = u; }
     __device__ u32x4 get(int i) const { return v[i]; }
-    static __device__ int at(int i, int q, int g, int G) { return 32 * ((2 * i + q / 2) * G + g) + 16 * (q % 2); }
-    u32x4 v[2];   // half h of group of(q / 2), then of of(2 + q / 2): the instruction's order of 8-bit operands
+    static __device__ int at(int i, int q, int g, int G) { return 32 * (q * G + g) + 16 * i; }
+    // Hides from the compiler that the values are the last tile's still, as it would convert
+    // them once for all: faster where that fits (64 x 4096 to 4096 9.5 us, 12.2 hidden), and
+    // spilled where not (64 x 8192 to 28672 254 us, 82 hidden).
+    __device__ void hide() { asm volatile("" : "+v"(v[0]), "+v"(v[1])); }
+    __device__ bf16x8 part(int j, int) const {
+        const uint32_t lo = v[j / 2][j % 2 * 2], hi = v[j / 2][j % 2 * 2 + 1];
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
+        const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+        const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
+        const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+        return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
     template <Ends ENDS, class Of>
     __device__ void load(const uint8_t* row, Of of, int q, int K) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int k = 32 * of(2 * h + q / 2) + 16 * (q % 2);
-            v[h] = load16<ENDS>(row, k, K);
-        }
+        for (int h = 0; h < 2; ++h) v[h] = load16<ENDS>(row, 32 * of(q) + 16 * h, K);
     }
 };
 
@@ -191,21 +178,9 @@ __device__ inline void multiply(const u32x4& codes, uint32_t power, const Fragme
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int c = 0; c < X::kParts; ++c)
-                acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[m].v[j][c], acc[m], 0, 0, 0);
+                acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x[m].part(j, c), acc[m], 0, 0, 0);
     }
 }
-template <int MT>
-__device__ inline void multiply(const u32x4& codes, uint32_t power, const Fragment<XFp8> (&x)[MT], f32x4 (&acc)[MT]) {
-    const i32x8 w{(int)codes[0], (int)codes[1], (int)codes[2], (int)codes[3], 0, 0, 0, 0};
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const i32x8 b{(int)x[m].v[0][0], (int)x[m].v[0][1], (int)x[m].v[0][2], (int)x[m].v[0][3],
-                      (int)x[m].v[1][0], (int)x[m].v[1][1], (int)x[m].v[1][2], (int)x[m].v[1][3]};
-        acc[m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, b, acc[m], 4 /* codes */, 0 /* e4m3 */, 0,
-                                                                (int)power, 0, 127);
-    }
-}
-
 template <class Y>
 __device__ inline void put(Y* p, float f);
 template <>
@@ -318,6 +293,16 @@ __global__ __launch_bounds__(kWaves * 64) void swr_fp4_kernel(Fp4Params p) {
     }
 }
 
+// Registers that a lane holds x in, and the most that it may.
+template <class X, int MT, int NB>
+constexpr int held() {
+    return (int)sizeof(Fragment<X>) / 4 * MT * NB;
+}
+constexpr int kMostHeld = 128;
+// Whether 8-bit x, made bf16, would not fit.
+template <class X, int MT, int NB>
+constexpr bool kHidden = std::is_same<X, XFp8>::value && 2 * held<X, MT, NB>() > kMostHeld;
+
 // The same with x in registers: a block's 8 waves share out k, each keeps what it
 // needs of x (NB blocks of 128 k) and takes the tiles of 16 rows of W in turn with the
 // other blocks, the next tile's codes on their way while one is worked on.
@@ -409,14 +394,19 @@ __global__ __launch_bounds__(kWaves * 64) void swr_fp4_held_kernel(Fp4Params p) 
     if (p.K % (16 / (int)sizeof(typename X::T)) == 0) hold(std::integral_constant<Ends, kEven>());
     else hold(std::integral_constant<Ends, kAny>());
     // A tile's sums of this wave.  The waves meet every TURNS tiles only, so that one may be
-    // ahead of another (16 x 8192 to 114688, 8-bit: 128 us with one, 120 with two, 115 with
-    // four; of bf16 141, 128, 121).
+    // ahead of another (16 x 8192 to 114688, bf16: 141 us with one, 128 with two, 121 with
+    // four).
     const auto work = [&](const Codes<X, NB>& c, int turn, int buf) {
         f32x4 acc[MT];
 #pragma unroll
         for (int t = 0; t < MT; ++t) acc[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int j = 0; j < NB; ++j) multiply(c.codes[j], c.power[j / G] >> 8 * (j % G) & 255, x[j], acc);
+        for (int j = 0; j < NB; ++j) {
+            if constexpr (kHidden<X, MT, NB>)
+#pragma unroll
+                for (int t = 0; t < MT; ++t) x[j][t].hide();
+            multiply(c.codes[j], c.power[j / G] >> 8 * (j % G) & 255, x[j], acc);
+        }
 #pragma unroll
         for (int t = 0; t < MT; ++t) join[buf][turn][wave][t][lane] = acc[t];
     };
@@ -504,13 +494,6 @@ hipError_t split(const Fp4Params& p, hipStream_t st) {
     return go<X, Y, R, MT, 8>(p, st);
 }
 
-// Registers that a lane holds x in, and the most that it may.
-template <class X, int MT, int NB>
-constexpr int held() {
-    return (int)sizeof(Fragment<X>) / 4 * MT * NB;
-}
-constexpr int kMostHeld = 128;
-
 template <class X, class Y, int MT, int NB>
 hipError_t hold(Fp4Params p, hipStream_t st) {
     if constexpr (held<X, MT, NB>() > kMostHeld) return hipErrorInvalidValue;   // (fits() is false)
@@ -518,8 +501,8 @@ hipError_t hold(Fp4Params p, hipStream_t st) {
         p.m_blocks = (p.M + 16 * MT - 1) / (16 * MT);
         const int64_t tiles = (p.N + 15) / 16, most = std::max(kCus / p.m_blocks, 1);
         // A second tile's codes on their way, where the registers have room for them
-        // (a third's gained 2 % at 16 x 8192 8-bit rows against 28672 and lost 1 % with bf16).
-        constexpr int depth = held<X, MT, NB>() + 2 * 5 * NB <= 224 ? 2 : 1;
+        // (a third's lost 1 % at 16 x 8192 bf16 rows against 28672).
+        constexpr int depth = held<X, MT, NB>() + 2 * 5 * NB + (kHidden<X, MT, NB> ? 32 : 0) <= 224 ? 2 : 1;
         hipLaunchKernelGGL((swr_fp4_held_kernel<X, Y, MT, NB, depth>),
                            dim3((unsigned)(std::min(tiles, most) * p.m_blocks)), dim3(kWaves * 64), 0, st, p);
         return hipGetLastError();
@@ -529,7 +512,7 @@ hipError_t hold(Fp4Params p, hipStream_t st) {
 // Blocks of 128 k of a wave, as the held kernel is built for them; 0 past its last.
 int blocks_a_wave(int K) {
     const int nb = ((K + 127) / 128 + kWaves - 1) / kWaves;
-    return nb <= 2 ? nb : nb <= 4 ? 4 : nb <= 6 ? 6 : nb <= 8 ? 8 : nb <= 16 ? 16 : 0;
+    return nb <= 2 ? nb : nb <= 4 ? 4 : nb <= 6 ? 6 : nb <= 8 ? 8 : 0;
 }
 
 template <class X, int MT>
@@ -545,22 +528,21 @@ hipError_t hold(const Fp4Params& p, hipStream_t st) {
         case 2: return hold<X, Y, MT, 2>(p, st);
         case 4: return hold<X, Y, MT, 4>(p, st);
         case 6: return hold<X, Y, MT, 6>(p, st);
-        case 8: return hold<X, Y, MT, 8>(p, st);
-        default: return hold<X, Y, MT, 16>(p, st);
+        default: return hold<X, Y, MT, 8>(p, st);
     }
 }
 
 // Which kernel, in us (split with one tile of W a wave, with two, held):
 //     rows of x     1000 to 1001     4096 to 4096     8192 to 8192        8192 to 28672
 //     1 bf16        4.5   -   4.2    5.0  6.7  6.3    12.2  13.3  14.4    46  41  36
-//     8 8-bit       4.4   -   4.4    5.1  6.5  4.8    14.4  10.6  11.7    42  40  33
+//     8 8-bit       4.4   -   4.4    5.1   -   4.8     -    13.3  13.0     -   -  35
 //     16 bf16        -    -    -     8.9  9.0  6.3    24.0  18.9  14.3    102 86  37
 //     5 float32     6.1   -   4.3     (does not fit)
 // The split kernel's lanes load x with a cache line for each of its rows, time after time; the
 // held one's load it once, but before all else, which few rows and few tiles pay back only
 // where x is short, of two blocks of 128 k a wave at most.  It has one block a CU (two: 10 %
-// slower).  Past 16 rows of x it takes 32 at a time if they fit (64 x 8192 to 28672,
-// 8-bit: 65 us, the split kernel 110).
+// slower).  Past 16 rows of x it takes 32 at a time if they fit (64 x 4096 to 4096,
+// bf16: 11.2 us, the split kernel 13.7).
 template <class X, class Y>
 hipError_t by_size(const Fp4Params& p, hipStream_t st) {
     const int tiles = (p.N + 15) / 16;
@@ -577,7 +559,7 @@ hipError_t by_size(const Fp4Params& p, hipStream_t st) {
 hipError_t launch_fp4(int dtype, int out_dtype, const Fp4Params& p, void* stream) {
     const hipStream_t st = (hipStream_t)stream;
     const bool f32 = out_dtype == SWR_DTYPE_F32;
-    if (dtype == SWR_DTYPE_FP8) return f32 ? by_size<XFp8Exact, float>(p, st) : by_size<XFp8, uint16_t>(p, st);
+    if (dtype == SWR_DTYPE_FP8) return f32 ? by_size<XFp8, float>(p, st) : by_size<XFp8, uint16_t>(p, st);
     if (dtype == SWR_DTYPE_BF16) return f32 ? by_size<XBf16, float>(p, st) : by_size<XBf16, uint16_t>(p, st);
     return f32 ? by_size<XF32, float>(p, st) : by_size<XF32, uint16_t>(p, st);
 }

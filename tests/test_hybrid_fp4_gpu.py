@@ -60,6 +60,27 @@ def test_linear(swr, dtype, M, N, K):
         _check(swr, x, codes, powers, scale, out)
 
 
+# Each way through the kernels: x held in registers of every length (one to sixteen blocks
+# of 128 k a wave), 16 and 32 rows at a time; several meetings of a workgroup's waves, the
+# last one short; x that does not fit; one tile of W a wave and two.
+LONG = [(9, 40, 1100), (12, 50, 3000), (16, 33, 4097), (10, 50, 6000), (16, 40, 8191), (11, 48, 16384), (10, 33, 16390),
+        (20, 40, 2049), (40, 35, 4000), (18, 47, 5200), (33, 18, 8192), (3, 20003, 40), (12, 8200, 300), (40, 9000, 300),
+        (17, 4500, 1500), (300, 5000, 100), (3, 4200, 2100), (8, 4099, 4500), (70, 4111, 2300)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32, FP8])
+@pytest.mark.parametrize("M,N,K", LONG)
+def test_long_rows_and_many_tiles(swr, dtype, M, N, K):
+    codes, powers = _weights(M + N + K, N, K)
+    x = _rows(K, M, K, dtype)
+    scale = torch.rand((M,), generator=torch.Generator().manual_seed(2)).cuda() + 0.1
+    y = _check(swr, x, codes, powers, scale)
+    _check(swr, x, codes, powers, None, F32)
+    again = swr.swr_fp4_linear(x, codes, powers, scale=scale)
+    torch.cuda.synchronize()
+    assert torch.equal(y, again)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32, FP8])
 def test_every_code_and_power(swr, dtype):
     # Row n of W has one group of one power, all 16 codes in it twice.
