@@ -148,8 +148,8 @@ __global__ __launch_bounds__(256) void swr_append_kernel(AppendParams p) {
 // holds column g = l of S at tokens 16 s + 4 u + i (s < 2, i < 4), which is where
 // the second product wants P: the order of its contraction index is free, so V's rows
 // are loaded for those tokens, and no lane exchanges P with another.  K and V go
-// from memory to registers, with no LDS between.  P is split into two
-// bf16 parts (float32 caches use float32 products throughout), so that y is
+// from memory to registers, with no LDS between.  Against bf16 values P is cut into three
+// bf16 parts, all 24 of its bits (float32 caches use float32 products throughout), so that y is
 // rounded once.  Maxima and sums are float32; a lane's sums are joined at the end.
 //
 // The work, (request, key head) rows of ceil(tokens / 32) tiles, is laid end to
@@ -378,11 +378,16 @@ struct State<B16, DP, FULL> {
 #pragma unroll
             for (int j = 0; j < CH; ++j) acc[j] *= alpha;
         }
-        bf16x8 hi, lo;
+        bf16x8 w[3];
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-            hi[t] = (__bf16)p[t];
-            lo[t] = (__bf16)(p[t] - (float)hi[t]);
+            // Cut off, not rounded: 8 bits each, and the differences are exact.
+            const uint32_t a = __builtin_bit_cast(uint32_t, p[t]) & 0xffff0000u;
+            const float r = p[t] - as_float(a);
+            const uint32_t b = __builtin_bit_cast(uint32_t, r) & 0xffff0000u;
+            w[0][t] = __builtin_bit_cast(__bf16, (uint16_t)(a >> 16));
+            w[1][t] = __builtin_bit_cast(__bf16, (uint16_t)(b >> 16));
+            w[2][t] = (__bf16)(r - as_float(b));
         }
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
@@ -392,9 +397,9 @@ struct State<B16, DP, FULL> {
             for (int t = 0; t < 4; ++t)
                 a[t] = __builtin_amdgcn_perm(x.v[2 * t + 1][j / 2], x.v[2 * t][j / 2],
                                              j % 2 ? 0x07060302u : 0x05040100u);
-            const bf16x8 w = __builtin_bit_cast(bf16x8, a);
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, hi, acc[j], 0, 0, 0);
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, lo, acc[j], 0, 0, 0);
+            const bf16x8 v = __builtin_bit_cast(bf16x8, a);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[i], acc[j], 0, 0, 0);
         }
     }
 };
