@@ -381,13 +381,17 @@ struct State<B16, DP, FULL> {
         bf16x8 w[3];
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-            // Cut off, not rounded: 8 bits each, and the differences are exact.
+            // Cut off, not rounded: 8 bits each, and the differences are exact and not
+            // negative.  The lower two are 2^-32 of the first at least (or the least bf16), far
+            // below p's own rounding: a zero times an infinite value would be NaN where p's is infinite.
             const uint32_t a = __builtin_bit_cast(uint32_t, p[t]) & 0xffff0000u;
+            const uint32_t least = (uint32_t)max((int)a - (32 << 23), 0x10000);
             const float r = p[t] - as_float(a);
             const uint32_t b = __builtin_bit_cast(uint32_t, r) & 0xffff0000u;
+            const uint32_t c = __builtin_bit_cast(uint32_t, r - as_float(b));
             w[0][t] = __builtin_bit_cast(__bf16, (uint16_t)(a >> 16));
-            w[1][t] = __builtin_bit_cast(__bf16, (uint16_t)(b >> 16));
-            w[2][t] = (__bf16)(r - as_float(b));
+            w[1][t] = __builtin_bit_cast(__bf16, (uint16_t)(max(b, least) >> 16));
+            w[2][t] = __builtin_bit_cast(__bf16, (uint16_t)(max(c, least) >> 16));
         }
 #pragma unroll
         for (int j = 0; j < CH; ++j) {

@@ -1,5 +1,5 @@
-"""What paged attention makes of its values: weights of all 24 bits, on both
-routes (a workgroup a row, and shares of the work)."""
+"""What paged attention makes of its values: weights of all 24 bits, infinite
+values, on both routes (a workgroup a row, and shares of the work)."""
 import math
 
 import pytest
@@ -69,3 +69,35 @@ def test_weights_keep_their_bits(swr, dtype, more):
     off = (f64(y) * (3 + p)[:, None, None]).abs().max()
     assert off <= (1.5 + 2 + 24 + 0.5) * 2.0 ** -24 * 1.01, off * 2 ** 24
     assert math.isfinite(off)
+
+
+@pytest.mark.parametrize("more", ROUTES)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_infinite_values(swr, dtype, more):
+    # An infinite value makes its channel of every head infinite, whatever its weight's bits:
+    # of a single token (a weight of 1), and of others; of both signs NaN.
+    lengths = [1, 2, 40, 300, 33, 64, 7]
+    kc, vc, table = _cache(lengths, 1, dtype, 40, heads=2, D=32)
+    q = torch.randn((len(lengths), 6, 32), generator=torch.Generator().manual_seed(2)).to(dtype).cuda()
+    run = lambda v: swr.swr_paged_attention(q, kc.cuda(), v.cuda(), _widened(table, more), _i32(lengths))
+    want = run(vc)
+    inf = float("inf")
+
+    def put(b, t, head, c, value):
+        vc[table[b, t // 16], t % 16, head, c] = value
+        y = want[b, 3 * head:3 * head + 3, c]
+        y[:] = value if (torch.isfinite(y) | (y == value)).all() else float("nan")
+
+    for b, n in enumerate(lengths):
+        for t in {0, n // 2, n - 1}:
+            put(b, t, 0, (5 * b + t) % 16, inf if t % 2 else -inf)
+            put(b, t, 1, 31 - t % 8, inf)
+    for t in (1, 2, 30, 31, 32, 200, 299):
+        put(3, t, 1, t % 20, -inf)
+    put(2, 3, 0, 17, inf)
+    put(2, 4, 0, 17, -inf)
+    got = run(vc)
+    torch.cuda.synchronize()
+    assert torch.isinf(want).any() and torch.isnan(want).any()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(nan=0.0, posinf=inf, neginf=-inf),
+                                                                            want.nan_to_num(nan=0.0, posinf=inf, neginf=-inf))
