@@ -198,7 +198,8 @@ typedef struct swr_paged {
  *     y[i, h] = sum_t p_t V[t] / sum_t p_t,   p_t = exp(scale q[i, h] . K[t])
  * over positions max(0, lengths[i] - window) .. lengths[i] - 1 and key head
  * h / (q_heads / heads).  A position whose page is not within the cache, or past
- * max_pages, is left out; a request with no position left has y = 0.
+ * max_pages, is left out; a request with no position left has y = 0 (one whose positions
+ * all have a product of -infinity has 0 / 0).
  * lse: NULL, or float32 [batch, q_heads] (contiguous) that receives log(sum_t p_t)
  * (-infinity for no position).  lengths and table are int32.  Products, softmax and sums in float32;
  * results do not depend on other requests beyond float32 rounding order. */

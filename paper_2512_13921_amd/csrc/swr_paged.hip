@@ -253,15 +253,19 @@ struct B32 {
 
 __device__ inline float as_float(uint32_t u) { return __builtin_bit_cast(float, u); }
 
+constexpr float kLowest = -3.402823466e38f;   // the least finite float
+
 // A column's running maximum (the same on its four lanes) and this lane's sum
-// of the weights against it.
+// of the weights against it.  The maximum is -infinity until a tile has a token, and
+// from then on kLowest at least: tokens whose scores are all -infinity leave a sum of 0, and
+// 0 / 0, but no token leaves y = 0.
 struct Running {
     float m = -INFINITY, sum = 0.0f;
 
-    // Scores (times log2 e) to weights against the running maximum; returns
-    // what the sums so far are multiplied by.
-    __device__ float weigh(float (&p)[8]) {
-        float top = m;
+    // Scores (times log2 e) of a tile with or without any tokens to weights against the
+    // running maximum; returns what the sums so far are multiplied by.
+    __device__ float weigh(float (&p)[8], bool any) {
+        float top = any ? fmaxf(m, kLowest) : m;
 #pragma unroll
         for (int t = 0; t < 8; ++t) top = fmaxf(top, p[t]);
         top = fmaxf(top, __shfl_xor(top, 16));
@@ -373,7 +377,7 @@ struct State<B16, DP, FULL> {
                     if (!in) x.v[t][j] = 0;
             }
         }
-        const float alpha = run.weigh(p);
+        const float alpha = run.weigh(p, x.valid != 0);
         if (__any(alpha != 1.0f)) {   // (the maximum seldom moves)
 #pragma unroll
             for (int j = 0; j < CH; ++j) acc[j] *= alpha;
@@ -383,9 +387,10 @@ struct State<B16, DP, FULL> {
         for (int t = 0; t < 8; ++t) {
             // Cut off, not rounded: 8 bits each, and the differences are exact and not
             // negative.  The lower two are 2^-32 of the first at least (or the least bf16), far
-            // below p's own rounding: a zero times an infinite value would be NaN where p's is infinite.
+            // below p's own rounding: a zero times an infinite value would be NaN where p's is
+            // infinite.  A weight of 0 stays 0.
             const uint32_t a = __builtin_bit_cast(uint32_t, p[t]) & 0xffff0000u;
-            const uint32_t least = (uint32_t)max((int)a - (32 << 23), 0x10000);
+            const uint32_t least = a ? (uint32_t)max((int)a - (32 << 23), 0x10000) : 0;
             const float r = p[t] - as_float(a);
             const uint32_t b = __builtin_bit_cast(uint32_t, r) & 0xffff0000u;
             const uint32_t c = __builtin_bit_cast(uint32_t, r - as_float(b));
@@ -482,7 +487,7 @@ struct State<B32, DP, FULL> {
                     if (!in) x.v[t][j] = 0.0f;
             }
         }
-        const float alpha = run.weigh(p);
+        const float alpha = run.weigh(p, x.valid != 0);
         if (__any(alpha != 1.0f)) {
 #pragma unroll
             for (int j = 0; j < CH; ++j) acc[j] *= alpha;
@@ -500,11 +505,11 @@ __device__ inline void put(float* y, float f) { *y = f; }
 
 constexpr float kLn2 = 0.69314718055994530942f;
 
-// Channel c of a row's output from its weighted sum and the weights' sum, which
-// is 0 where the row has no token (a token of the maximum weighs 1).
+// Channel c of a row's output from its maximum, weighted sum and weights' sum; the
+// maximum is -infinity where the row has no token.
 template <class T>
 __device__ inline void finish(const PagedParams& p, int b, int64_t head, int c, float m, float y, float sum) {
-    if (c < p.D) put((T*)p.y + b * p.sy_b + head * p.sy_h + c, sum == 0.0f ? 0.0f : y / sum);
+    if (c < p.D) put((T*)p.y + b * p.sy_b + head * p.sy_h + c, m == -INFINITY ? 0.0f : y / sum);
     if (c == 0 && p.lse)
         p.lse[(int64_t)b * p.kv_heads * p.group + head] = sum == 0.0f ? -INFINITY : (m + log2f(sum)) * kLn2;
 }
@@ -608,7 +613,7 @@ __device__ inline void attend(const PagedParams& p, const Rows& r, int b, int h,
 template <class T>
 __device__ inline void nothing(const PagedParams& p, int b, int64_t head, int columns) {
     for (int e = threadIdx.x; e < columns * p.D; e += blockDim.x)
-        finish<T>(p, b, head + e / p.D, e % p.D, 0.0f, 0.0f, 0.0f);
+        finish<T>(p, b, head + e / p.D, e % p.D, -INFINITY, 0.0f, 0.0f);
 }
 
 // Waves of the kernel below that a SIMD holds (a compute unit as many blocks).

@@ -1,5 +1,5 @@
 """What paged attention makes of its values: weights of all 24 bits, infinite
-values, on both routes (a workgroup a row, and shares of the work)."""
+values, scores of -infinity, on both routes (a workgroup a row, and shares of the work)."""
 import math
 
 import pytest
@@ -101,3 +101,33 @@ def test_infinite_values(swr, dtype, more):
     assert torch.isinf(want).any() and torch.isnan(want).any()
     assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(nan=0.0, posinf=inf, neginf=-inf),
                                                                             want.nan_to_num(nan=0.0, posinf=inf, neginf=-inf))
+
+
+@pytest.mark.parametrize("more", ROUTES)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_scores_of_minus_infinity(swr, dtype, more):
+    # Tokens of such scores weigh nothing (as those of very low ones do); where a request has no
+    # others, y is 0 / 0 and the sum's logarithm -infinity.  Only a request without a position has y = 0.
+    lengths = [1, 40, 300, 1000, 1000, 64, 0, 20]
+    kc, vc, table = _cache(lengths, 3, dtype, 160, heads=1, D=64)
+    q = torch.randn((len(lengths), 3, 64), generator=torch.Generator().manual_seed(4))
+    q[..., 0] = q[..., 0].abs().clamp(0.1, 1)
+    q = q.to(dtype).cuda()
+    spots = {b: range(n) for b, n in enumerate(lengths) if b in (0, 2, 3)}     # all of a request's tokens
+    spots.update({1: range(32), 4: list(range(600)) + [999], 5: [63]})         # its first, most, its last
+    table[7] = -1                                                              # tokens on no page: no position
+    run = lambda k: swr.swr_paged_attention(q, k.cuda(), vc.cuda(), _widened(table, more), _i32(lengths), want_lse=True)
+    low = kc.clone()
+    for b, at in spots.items():
+        for t in at:
+            kc[table[b, t // 16], t % 16, 0, 0], low[table[b, t // 16], t % 16, 0, 0] = float("-inf"), -1e38
+    y, lse = run(kc)
+    want, wl = run(low)
+    torch.cuda.synchronize()
+    for b, n in enumerate(lengths):
+        if b in (0, 2, 3):
+            assert torch.isnan(y[b]).all() and (lse[b] == float("-inf")).all(), b
+        elif n == 0 or b == 7:
+            assert (y[b] == 0).all() and (lse[b] == float("-inf")).all(), b
+        else:
+            assert torch.equal(y[b], want[b]) and torch.equal(lse[b], wl[b]) and torch.isfinite(y[b]).all(), b
