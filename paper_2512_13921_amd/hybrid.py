@@ -456,12 +456,16 @@ def _autograd_function():
 
     class _SWRNormFunction(torch.autograd.Function):
         """Autograd wrapper of the norm with its residual: (y, h) of (x, weight,
-        residual, eps); only h and the weight are kept for the backward."""
+        residual, eps); only h and the weight are kept for the backward.  Without a
+        residual (None) h is x."""
 
         @staticmethod
         def forward(ctx, x, weight, residual, eps=1e-6):
-            y, h = swr_rms_norm(x, weight, residual=residual, eps=eps)
-            ctx.eps = eps
+            if residual is None:
+                y, h = swr_rms_norm(x, weight, eps=eps), x
+            else:
+                y, h = swr_rms_norm(x, weight, residual=residual, eps=eps)
+            ctx.eps, ctx.has_residual = eps, residual is not None
             ctx.save_for_backward(h, weight)
             return y, h
 
@@ -469,7 +473,7 @@ def _autograd_function():
         def backward(ctx, dy, dh):
             h, weight = ctx.saved_tensors
             dx, dw = swr_rms_norm_backward(h, weight, dy, dh=dh, eps=ctx.eps)
-            return dx, dw.to(weight.dtype), dx, None
+            return dx, dw.to(weight.dtype), dx if ctx.has_residual else None, None
 
     return _SWRNormFunction
 
