@@ -451,6 +451,16 @@ def swr_paged_attention(q, k_cache, v_cache, block_table, lengths, scale=None, w
 # ----------------------------------------------------------------------------- autograd
 
 
+def _as_rows(g):
+    """A gradient as it comes, or a copy where the calls cannot take its layout (an
+    expanded or a transposed one)."""
+    try:
+        _rows(g, "gradient")
+    except ValueError:
+        return g.contiguous()
+    return g
+
+
 def _autograd_function():
     torch = _torch()
 
@@ -472,7 +482,7 @@ def _autograd_function():
         @staticmethod
         def backward(ctx, dy, dh):
             h, weight = ctx.saved_tensors
-            dx, dw = swr_rms_norm_backward(h, weight, dy, dh=dh, eps=ctx.eps)
+            dx, dw = swr_rms_norm_backward(h, weight, _as_rows(dy), dh=_as_rows(dh), eps=ctx.eps)
             return dx, dw.to(weight.dtype), dx if ctx.has_residual else None, None
 
     return _SWRNormFunction

@@ -1,5 +1,5 @@
-"""The norm under autograd: with and without a residual, against the 64-bit
-form."""
+"""The norm under autograd: with and without a residual, and with gradients of any
+layout that autograd passes, against the 64-bit form."""
 import pytest
 
 import hybrid_ref as ref
@@ -55,3 +55,49 @@ def test_with_a_residual(swr, dtype, shape):
     dx, dr, dw = torch.autograd.grad((y, h), (x, r, w), (gy, gh))
     _check_gradients(h.detach(), w.detach(), gy, gh, dx, dw)
     assert torch.equal(dx, dr)
+
+
+def _layouts(shape, dtype):
+    """Gradients of a shape as autograd passes them: expanded, transposed, of steps and
+    in an order whose rows are no run."""
+    yield "expanded", _rand(10, (1,) * len(shape), dtype).expand(shape)
+    yield "a row for all", _rand(11, shape[-1:], dtype).expand(shape)
+    yield "a value a row", _rand(12, (*shape[:-1], 1), dtype).expand(shape)
+    yield "transposed", _rand(13, (*shape[:-2], shape[-1], shape[-2]), dtype).transpose(-1, -2)
+    yield "every second channel", _rand(14, (*shape[:-1], 2 * shape[-1]), dtype)[..., ::2]
+    if len(shape) > 2:
+        yield "batch inside", _rand(15, (*shape[1:-1], shape[0], shape[-1]), dtype).movedim(-2, 0)
+    if len(shape) == 4:
+        yield "swapped", _rand(16, (shape[2], shape[1], shape[0], shape[3]), dtype).permute(2, 1, 0, 3)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shape", [(6, 40), (2, 5, 64), (3, 2, 4, 48)])
+@pytest.mark.parametrize("with_residual", [True, False])
+def test_gradients_of_any_layout(swr, dtype, shape, with_residual):
+    x, w = _rand(17, shape, dtype).requires_grad_(True), _rand(18, shape[-1:], dtype).requires_grad_(True)
+    r = _rand(19, shape, dtype) if with_residual else None
+    dense = _rand(20, shape, dtype)
+    for what, g in _layouts(shape, dtype):
+        for gy, gh in ((g, dense), (dense, g), (g, g)):
+            y, h = swr.SWRNormFunction.apply(x, w, r)
+            dx, dw = torch.autograd.grad((y, h), (x, w), (gy, gh))
+            y, h = swr.SWRNormFunction.apply(x, w, r)
+            want = torch.autograd.grad((y, h), (x, w), (gy.contiguous(), gh.contiguous()))
+            assert torch.equal(dx, want[0]) and torch.equal(dw, want[1]), what
+            _check_gradients(h.detach(), w.detach(), gy, gh, dx, dw)
+
+
+@pytest.mark.parametrize("loss", [lambda y, h: y.sum(), lambda y, h: h.mean(), lambda y, h: y.sum() + h.sum(),
+                                  lambda y, h: (y.transpose(0, 1) @ h).sum()])
+def test_ordinary_losses(swr, loss):
+    x, r, w = (_rand(i, s, F32).requires_grad_(True) for i, s in ((21, (7, 33)), (22, (7, 33)), (23, (33,))))
+    y, h = swr.SWRNormFunction.apply(x, w, r)
+    loss(y, h).backward()
+    plain = [t.detach().double().requires_grad_(True) for t in (x, w, r)]
+    s = plain[0] + plain[2]
+    loss(s * torch.rsqrt(s.square().mean(-1, keepdim=True) + 1e-6) * plain[1], s).backward()
+    for got, want in zip((x, w, r), plain):
+        want = torch.zeros_like(want) if want.grad is None else want.grad     # (h does not depend on the weight)
+        # sums of 33 or 7 float32 terms of a few units, of a product of two matrices at most
+        assert (got.grad.double() - want).abs().max() <= 2e-5 * (1 + want.abs().max())
