@@ -68,7 +68,8 @@ typedef struct swr_norm {
     int64_t sy_o, sy_i;        /* ... of y (the backward's dy)                             */
 } swr_norm_t;
 
-/* Forward.  residual and h may be NULL (without a residual, h is a copy of x).
+/* Forward.  residual and h may be NULL (without a residual, h is a copy of x), and then
+ * their strides are not read; so may the backward's dh.
  * With out_dtype SWR_DTYPE_FP8, y holds q and scale [outer * inner] float32
  * receives s, with  s = max|y| / 448  over the row and  q = y / s  rounded to
  * nearest even (a row of zeros has s = 0 and q = 0; a row that holds a NaN has

@@ -496,7 +496,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* v, Py_ssize_t) {
     if (!g.ok) return none();
     if (fp8) n.out_dtype = SWR_DTYPE_FP8;
     dense_rows(n, &n.sy_o, &n.sy_i);
-    dense_rows(n, &n.sh_o, &n.sh_i);
+    if (r.defined()) dense_rows(n, &n.sh_o, &n.sh_i);
     at::Tensor y, s, h;
     int rc;
     {

@@ -125,7 +125,8 @@ bool meet(const swr_norm_t* n, const RowTensor& a, const RowTensor& b) {
     return false;
 }
 
-int resolve(const swr_norm_t* n, bool backward, Rows* out) {
+// (Strides of tensors that a call does not have are not looked at: r is the residual, or dh.)
+int resolve(const swr_norm_t* n, bool backward, bool has_r, bool has_h, Rows* out) {
     if (!n) return SWR_ERR_NULL;
     if (n->abi_version != SWR_ABI_VERSION) return SWR_ERR_VERSION;
     if (!plain(n->dtype) || (n->weight_dtype != n->dtype && n->weight_dtype != SWR_DTYPE_F32)) return SWR_ERR_DTYPE;
@@ -145,8 +146,8 @@ int resolve(const swr_norm_t* n, bool backward, Rows* out) {
         return off < kMaxExtent / 8;
     };
     const bool ok = bytes(n->sx_o, n->sx_i, out->es, false, &out->x) &&
-                    bytes(n->sr_o, n->sr_i, out->es, false, &out->r) &&
-                    bytes(n->sh_o, n->sh_i, out->es, true, &out->h) &&
+                    (!has_r || bytes(n->sr_o, n->sr_i, out->es, false, &out->r)) &&
+                    (!has_h || bytes(n->sh_o, n->sh_i, out->es, true, &out->h)) &&
                     bytes(n->sy_o, n->sy_i, size_of(n->out_dtype), !backward, &out->y);
     return ok ? SWR_OK : SWR_ERR_SHAPE;
 }
@@ -181,8 +182,8 @@ extern "C" {
 
 int swr_rms_norm(const swr_norm_t* n, const void* x, const void* residual, const void* weight, void* y, float* scale,
                  void* h, void* stream) {
-    Rows r;
-    const int rc = resolve(n, false, &r);
+    Rows r = {};
+    const int rc = resolve(n, false, residual != nullptr, h != nullptr, &r);
     if (rc != SWR_OK) return rc;
     if (r.empty) return SWR_OK;
     const bool fp8 = n->out_dtype == SWR_DTYPE_FP8;
@@ -203,8 +204,8 @@ int swr_rms_norm(const swr_norm_t* n, const void* x, const void* residual, const
 }
 
 int64_t swr_rms_norm_workspace_bytes(const swr_norm_t* n) {
-    Rows r;
-    const int rc = resolve(n, true, &r);
+    Rows r = {};
+    const int rc = resolve(n, true, false, true, &r);
     if (rc != SWR_OK) return rc;
     if (r.empty) return 0;
     const swr::NormPlan plan = swr::plan_norm(n->dtype, r.rows, n->width, true);
@@ -213,8 +214,8 @@ int64_t swr_rms_norm_workspace_bytes(const swr_norm_t* n) {
 
 int swr_rms_norm_backward(const swr_norm_t* n, const void* h, const void* weight, const void* dy, const void* dh,
                           void* dx, float* dweight, void* workspace, void* stream) {
-    Rows r;
-    const int rc = resolve(n, true, &r);
+    Rows r = {};
+    const int rc = resolve(n, true, dh != nullptr, true, &r);
     if (rc != SWR_OK) return rc;
     if (!dweight) return SWR_ERR_NULL;
     if (!aligned(dweight, 4)) return SWR_ERR_ALIGN;

@@ -212,8 +212,6 @@ def swr_rms_norm(x, weight, residual=None, eps=1e-6, fp8=False, y=None, h=None, 
         if h is None:
             h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         n.sh_o, n.sh_i = _same(x, h, "h")
-    else:
-        n.sh_o, n.sh_i = n.inner * n.width, n.width   # (not stored)
     scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if fp8 else None
     _check(_lib().swr_rms_norm(ctypes.byref(n), _ptr(x), _opt(residual), _ptr(weight), _ptr(y), _opt(scale), _opt(h),
                                _stream(stream, x.device)), "swr_rms_norm")
