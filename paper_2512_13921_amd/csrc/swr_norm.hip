@@ -469,64 +469,68 @@ __global__ __launch_bounds__(1024) void swr_norm_stats_kernel(NormParams p) {
     }
 }
 
-// Second walk: a block takes 256 vectors of columns (blockIdx.y) of every
-// gridDim.x-th row.
+// Second walk: a block takes 256 vectors of columns (blockIdx.y and every gridDim.y-th) of
+// every gridDim.x-th row.
 template <class E, class WE>
 __global__ __launch_bounds__(256) void swr_norm_bwd_wide_kernel(NormParams p) {
     constexpr int NE = E::NE;
     typedef typename E::store T;
     typedef typename WE::store WT;
-    const int64_t e = ((int64_t)blockIdx.y * 256 + threadIdx.x) * NE;
-    if (e >= p.width) return;
-    const int n = p.width - (int)e;
-    float w[NE], dw[NE] = {};
-    load<WE, NE>((const WT*)p.w, (int)e, p.width, w);
-    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
-        const float2 s = p.stats[row];
-        float h[NE], d[NE], f[NE] = {};
-        load<E, NE>((const T*)p.x + row_offset(row, p.inner, p.sx_o, p.sx_i), (int)e, p.width, h);
-        load<E, NE>((const T*)p.y + row_offset(row, p.inner, p.sy_o, p.sy_i), (int)e, p.width, d);
-        if (p.r) load<E, NE>((const T*)p.r + row_offset(row, p.inner, p.sr_o, p.sr_i), (int)e, p.width, f);
+    for (int64_t e = ((int64_t)blockIdx.y * 256 + threadIdx.x) * NE; e < p.width; e += (int64_t)gridDim.y * 256 * NE) {
+        const int n = p.width - (int)e;
+        float w[NE], dw[NE] = {};
+        load<WE, NE>((const WT*)p.w, (int)e, p.width, w);
+        for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+            const float2 s = p.stats[row];
+            float h[NE], d[NE], f[NE] = {};
+            load<E, NE>((const T*)p.x + row_offset(row, p.inner, p.sx_o, p.sx_i), (int)e, p.width, h);
+            load<E, NE>((const T*)p.y + row_offset(row, p.inner, p.sy_o, p.sy_i), (int)e, p.width, d);
+            if (p.r) load<E, NE>((const T*)p.r + row_offset(row, p.inner, p.sr_o, p.sr_i), (int)e, p.width, f);
 #pragma unroll
-        for (int i = 0; i < NE; ++i) {
-            f[i] += s.x * (d[i] * w[i] - h[i] * s.y);
-            dw[i] += d[i] * (h[i] * s.x);
+            for (int i = 0; i < NE; ++i) {
+                f[i] += s.x * (d[i] * w[i] - h[i] * s.y);
+                dw[i] += d[i] * (h[i] * s.x);
+            }
+            store<E, NE>((T*)p.h + row_offset(row, p.inner, p.sh_o, p.sh_i) + e, n, f);
         }
-        store<E, NE>((T*)p.h + row_offset(row, p.inner, p.sh_o, p.sh_i) + e, n, f);
+        store<F32, NE>(p.partial + (int64_t)blockIdx.x * p.width + e, n, dw);
     }
-    store<F32, NE>(p.partial + (int64_t)blockIdx.x * p.width + e, n, dw);
 }
 
-// dw: the sum of `blocks` rows of partial.  A block takes 16 columns, its 64
-// groups of 16 threads every 64th row, then the groups are added in order.
+// dw: the sum of `blocks` rows of partial.  A block takes 16 columns (and 16 of every gridDim.x
+// times 16 more), its 64 groups of 16 threads every 64th row, then the groups are added in order.
 __global__ __launch_bounds__(1024) void swr_norm_dw_kernel(const float* partial, float* dw, int width, int blocks) {
     __shared__ float buf[64][16];
     const int c = threadIdx.x % 16, group = threadIdx.x / 16;
-    const int64_t col = (int64_t)blockIdx.x * 16 + c;
-    float s = 0.0f;
-    if (col < width) {
+    for (int64_t first = (int64_t)blockIdx.x * 16; first < width; first += (int64_t)gridDim.x * 16) {
+        const int64_t col = first + c;
+        float s = 0.0f;
+        if (col < width) {
 #pragma unroll 8
-        for (int b = group; b < blocks; b += 64) s += partial[(int64_t)b * width + col];
-    }
-    buf[group][c] = s;
-    __syncthreads();
-    if (group < 8) {
-        s = 0.0f;
+            for (int b = group; b < blocks; b += 64) s += partial[(int64_t)b * width + col];
+        }
+        buf[group][c] = s;
+        __syncthreads();
+        if (group < 8) {
+            s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s += buf[8 * group + i][c];
-        buf[8 * group][c] = s;
-    }
-    __syncthreads();
-    if (group == 0 && col < width) {
-        s = 0.0f;
+            for (int i = 0; i < 8; ++i) s += buf[8 * group + i][c];
+            buf[8 * group][c] = s;
+        }
+        __syncthreads();
+        if (group == 0 && col < width) {
+            s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s += buf[8 * i][c];
-        dw[col] = s;
+            for (int i = 0; i < 8; ++i) s += buf[8 * i][c];
+            dw[col] = s;
+        }
+        __syncthreads();   // (the sums have been read)
     }
 }
 
 constexpr int64_t kFewRows = 512;          // rows that leave a compute unit two or fewer: latency counts
-constexpr int64_t kMostBlocks = 1 << 20;   // of a forward launch, whose blocks take rows in turn
+constexpr int64_t kMostBlocks = 1 << 20;   // of a launch in x, whose blocks take rows (or columns) in turn
+constexpr unsigned kMostColumns = 1 << 15; // of a launch in y, whose blocks take columns in turn
 
 unsigned grid_of(int64_t blocks) { return (unsigned)std::min(blocks, kMostBlocks); }
 
@@ -591,7 +595,7 @@ hipError_t backward(const NormPlan& plan, const NormParams& p, hipStream_t st) {
     } else if (plan.vpt == 0) {
         hipLaunchKernelGGL((swr_norm_stats_kernel<E, WE>), dim3(grid_of(p.rows)), dim3(1024), 0, st, p);
         if ((e = hipGetLastError()) != hipSuccess) return e;
-        const unsigned cols = (unsigned)((p.width + 256 * E::NE - 1) / (256 * E::NE));
+        const unsigned cols = std::min((unsigned)((p.width + 256 * E::NE - 1) / (256 * E::NE)), kMostColumns);
         hipLaunchKernelGGL((swr_norm_bwd_wide_kernel<E, WE>), dim3((unsigned)plan.blocks, cols), dim3(256), 0, st, p);
         e = hipGetLastError();
     } else {
@@ -599,7 +603,7 @@ hipError_t backward(const NormPlan& plan, const NormParams& p, hipStream_t st) {
                        : by_vectors<2>(plan.vpt, Backward<E, WE, false>{plan, p, st});
     }
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(swr_norm_dw_kernel, dim3((unsigned)((p.width + 15) / 16)), dim3(1024), 0, st, p.partial, p.dw,
+    hipLaunchKernelGGL(swr_norm_dw_kernel, dim3(grid_of((p.width + 15) / 16)), dim3(1024), 0, st, p.partial, p.dw,
                        p.width, plan.blocks);
     return hipGetLastError();
 }
