@@ -179,7 +179,8 @@ typedef struct swr_cache {
 
 /* New keys and values into their slots: k and v are [tokens, heads, D] with
  * strides sk[0..1] and sv[0..1] (token, head), slots int64 [tokens].  A token whose
- * slot is not within the cache is left out; the slots of one call are distinct. */
+ * slot is not within the cache is left out; the slots of one call are distinct.  The two
+ * caches may be parts of one allocation, between each other's elements. */
 int swr_cache_append(const swr_cache_t* cache, int64_t tokens, const int64_t* sk, const int64_t* sv, const void* k,
                      const void* v, const int64_t* slots, void* k_cache, void* v_cache, void* stream);
 

@@ -34,25 +34,44 @@ int64_t max_offset(std::initializer_list<Dim> dims) {
     return off;
 }
 
-// Whether different indices never name the same element.
-bool apart(std::initializer_list<Dim> dims) {
+// Dimensions (up to four) of more than one element, of the least stride first.
+struct Sorted {
     Dim d[4];
     int n = 0;
-    for (const Dim& x : dims)
-        if (x.size > 1) d[n++] = x;
-    for (int i = 1; i < n; ++i)
-        for (int j = i; j > 0 && d[j].stride < d[j - 1].stride; --j) {
-            const Dim t = d[j];
-            d[j] = d[j - 1];
-            d[j - 1] = t;
-        }
+    explicit Sorted(std::initializer_list<Dim> dims) {
+        for (const Dim& x : dims)
+            if (x.size > 1) d[n++] = x;
+        for (int i = 1; i < n; ++i)
+            for (int j = i; j > 0 && d[j].stride < d[j - 1].stride; --j) {
+                const Dim t = d[j];
+                d[j] = d[j - 1];
+                d[j - 1] = t;
+            }
+    }
+};
+
+// Whether different indices never name the same element.
+bool apart(std::initializer_list<Dim> dims) {
+    const Sorted s(dims);
     int64_t need = 1;
-    for (int i = 0; i < n; ++i) {
-        if (d[i].stride < need) return false;
-        if (d[i].size > kMaxExtent / d[i].stride) return false;
-        need = d[i].stride * d[i].size;
+    for (int i = 0; i < s.n; ++i) {
+        if (s.d[i].stride < need) return false;
+        if (s.d[i].size > kMaxExtent / s.d[i].stride) return false;
+        need = s.d[i].stride * s.d[i].size;
     }
     return true;
+}
+
+// Whether two tensors of these dimensions, apart, share an element when they begin
+// `distance` elements from each other.  The lesser dimensions reach less far than a
+// dimension's stride, so only its two differences of indices next to the distance count.
+bool meet_at(const Sorted& s, int dims, int64_t distance) {
+    if (dims == 0) return distance == 0;
+    const Dim& d = s.d[dims - 1];
+    const int64_t below = distance / d.stride - (distance % d.stride < 0);
+    for (int64_t i = below; i <= below + 1; ++i)
+        if (i > -d.size && i < d.size && meet_at(s, dims - 1, distance - i * d.stride)) return true;
+    return false;
 }
 
 struct Span {
@@ -97,32 +116,15 @@ struct Rows {
 
 // Whether two tensors of the norm's rows share an element.  Those of the same
 // strides and type, as parts of one larger tensor are, may lie between each
-// other's rows: they meet only where their distance is within a row of a
-// difference of two row positions, and rows being apart, only the
-// nearest such differences count.  Others are taken to meet where their spans do.
+// other's rows; others are taken to meet where their spans do.
 bool meet(const swr_norm_t* n, const RowTensor& a, const RowTensor& b) {
     const Span sa = span(a.p, a.bytes), sb = span(b.p, b.bytes);
     if (!overlap(sa, sb)) return false;
     const int64_t distance = (int64_t)(sb.lo - sa.lo);
-    const Dim outer{n->outer, a.so}, inner{n->inner, a.si};
-    if (a.so != b.so || a.si != b.si || a.es != b.es || distance % a.es != 0 ||
-        !apart({outer, inner, {n->width, 1}}))
-        return true;
-    const bool swap = outer.size <= 1 || (inner.size > 1 && inner.stride > outer.stride);
-    const Dim big = swap ? inner : outer, small = swap ? outer : inner;
-    const int64_t d = distance / a.es;
-    const int64_t i0 = big.size > 1 ? d / big.stride : 0;
-    for (int64_t i = i0 - 1; i <= i0 + 1; ++i) {
-        if (i <= -big.size || i >= big.size) continue;
-        const int64_t e = big.size > 1 ? d - i * big.stride : d;
-        const int64_t j0 = small.size > 1 ? e / small.stride : 0;
-        for (int64_t j = j0 - 1; j <= j0 + 1; ++j) {
-            if (j <= -small.size || j >= small.size) continue;
-            const int64_t f = small.size > 1 ? e - j * small.stride : e;
-            if (f > -n->width && f < n->width) return true;
-        }
-    }
-    return false;
+    const std::initializer_list<Dim> dims = {{n->outer, a.so}, {n->inner, a.si}, {n->width, 1}};
+    if (a.so != b.so || a.si != b.si || a.es != b.es || distance % a.es != 0 || !apart(dims)) return true;
+    const Sorted s(dims);
+    return meet_at(s, s.n, distance / a.es);
 }
 
 // (Strides of tensors that a call does not have are not looked at: r is the residual, or dh.)
@@ -383,7 +385,9 @@ int swr_cache_append(const swr_cache_t* c, int64_t tokens, const int64_t* sk, co
         return SWR_ERR_ALIGN;
     const Span in[3] = {span(k, (ok + 1) * es), span(v, (ov + 1) * es), span(slots, tokens * 8)};
     const Span out[2] = {span(k_cache, bytes), span(v_cache, bytes)};
-    if (overlap(out[0], out[1])) return SWR_ERR_ALIAS;
+    // The two caches may be parts of one allocation, between each other's elements.
+    const Sorted dims({{c->pages, c->s_page}, {c->page_size, c->s_token}, {c->heads, c->s_head}, {c->D, 1}});
+    if (overlap(out[0], out[1]) && meet_at(dims, dims.n, (int64_t)(out[1].lo - out[0].lo) / es)) return SWR_ERR_ALIAS;
     for (const Span& s : in)
         if (overlaps(s, {out[0], out[1]})) return SWR_ERR_ALIAS;
     const int64_t unit = 16 / es;
