@@ -170,6 +170,7 @@ constexpr int kWaves = 4;
 // 9.4 us, 13.2 in shares; of 1000 15.1 and 13.5, of 1500 20.3 and 14.0.  256 rows gain past it
 // if they are alike, 1500 tokens 42 and 50, and lose if not, 17 to 2000 tokens 27.6 and 23.3.)
 constexpr int kShort = 1024;
+constexpr int64_t kMostRows = 1 << 23;   // (a launch has fewer than 2^32 threads, a row 512 of them)
 // Shares of the work: three workgroups a compute unit, which is what a unit
 // holds of heads of up to 256 bytes.  Not a power of two: of equal rows, whose
 // lengths mostly are, shares would begin at multiples of large powers of two and so
@@ -789,8 +790,8 @@ hipError_t by_width(const PagedParams& p, hipStream_t st) {
 int paged_workgroups(const swr_paged_t& p) {
     const int64_t table = p.max_pages * p.cache.page_size;
     const int64_t positions = p.window > 0 ? std::min(p.window, table) : table;
-    if (positions <= kShort) return 0;
     const int64_t heads = p.cache.heads * ((p.q_heads / p.cache.heads + 15) / 16);
+    if (positions <= kShort && p.batch * heads < kMostRows) return 0;
     const double tiles = (double)p.batch * (double)heads * (double)((positions + kTile - 1) / kTile);
     return (int)std::min((double)kShares, (tiles + kWaves - 1) / kWaves);
 }
