@@ -474,8 +474,7 @@ template <class X, class Y, int R, int MT, int WK>
 hipError_t go(Fp4Params p, hipStream_t st) {
     constexpr int rows = 16 * R * (kWaves / WK), ahead = MT == 1 ? 2 : 1;
     p.m_blocks = (p.M + 16 * MT - 1) / (16 * MT);
-    const int64_t blocks = (int64_t)((p.N + rows - 1) / rows) * p.m_blocks;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    const int64_t blocks = (int64_t)((p.N + rows - 1) / rows) * p.m_blocks;   // (at most kMostTiles)
     hipLaunchKernelGGL((swr_fp4_kernel<X, Y, R, MT, kGroups, WK, ahead>), dim3((unsigned)blocks), dim3(kWaves * 64), 0,
                        st, p);
     return hipGetLastError();
@@ -554,9 +553,31 @@ hipError_t by_size(const Fp4Params& p, hipStream_t st) {
     return tiles <= kCus ? split<X, Y, 1, 1>(p, st) : split<X, Y, 2, 1>(p, st);
 }
 
+constexpr int64_t kMostTiles = (1 << 23) - 1;   // of y, 16 x 16, a block of 512 threads each at most: below 2^32 threads
+
 }  // namespace
 
 hipError_t launch_fp4(int dtype, int out_dtype, const Fp4Params& p, void* stream) {
+    const int64_t m = ((int64_t)p.M + 15) / 16, n = ((int64_t)p.N + 15) / 16;
+    if (m * n > kMostTiles) {   // y in two halves
+        Fp4Params a = p, b = p;
+        const int64_t half = (std::max(m, n) + 1) / 2 * 16, es = out_dtype == SWR_DTYPE_F32 ? 4 : 2;
+        if (m >= n) {
+            a.M = (int32_t)half;
+            b.M -= a.M;
+            b.x = (const char*)p.x + half * p.sx * (dtype == SWR_DTYPE_F32 ? 4 : dtype == SWR_DTYPE_BF16 ? 2 : 1);
+            if (p.scale) b.scale += half;
+            b.y = (char*)p.y + half * p.sy * es;
+        } else {
+            a.N = (int32_t)half;
+            b.N -= a.N;
+            b.codes += half * p.sc;
+            b.powers += half * p.sp;
+            b.y = (char*)p.y + half * es;
+        }
+        const hipError_t e = launch_fp4(dtype, out_dtype, a, stream);
+        return e != hipSuccess ? e : launch_fp4(dtype, out_dtype, b, stream);
+    }
     const hipStream_t st = (hipStream_t)stream;
     const bool f32 = out_dtype == SWR_DTYPE_F32;
     if (dtype == SWR_DTYPE_FP8) return f32 ? by_size<XFp8, float>(p, st) : by_size<XFp8, uint16_t>(p, st);

@@ -41,3 +41,21 @@ def test_attention_of_more_short_rows_than_a_launch_has_blocks(swr):
         # bf16's rounding; scores of 16 products of a few units
         worst = max(worst, float(((y[at].double() - want).abs() - want.abs() * 2.0 ** -8).max()))
     assert worst <= 1e-5
+
+
+@pytest.mark.parametrize("M,N", [((1 << 28) + 37, 1), (3, (1 << 27) + 21), ((1 << 22) + 3, 600)])
+def test_products_of_more_tiles_than_a_launch_has_blocks(swr, M, N):
+    # y of more than 2^23 tiles of 16 x 16, each the product of one weight and one value.
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn((M, 1), generator=g, device="cuda").to(FP8)
+    scale = torch.rand((M,), generator=g, device="cuda") + 0.5
+    codes = torch.zeros((N, 16), dtype=torch.uint8, device="cuda")
+    codes[:, 0] = torch.randint(0, 16, (N,), generator=g, device="cuda", dtype=torch.uint8)
+    powers = torch.randint(120, 130, (N, 1), generator=g, device="cuda", dtype=torch.uint8)
+    y = swr.swr_fp4_linear(x, codes, powers, scale=scale)
+    sizes = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device="cuda")
+    w = torch.cat([sizes, -sizes])[codes[:, 0].int()] * torch.exp2(powers[:, 0].float() - 127)
+    step = max(1, (1 << 26) // N)
+    for m in range(0, M, step):     # exact products, rounded once by the scale's and once to bf16
+        want = ((x[m:m + step].float() * w) * scale[m:m + step, None]).to(BF16)
+        assert torch.equal(y[m:m + step], want), m
