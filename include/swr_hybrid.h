@@ -192,7 +192,7 @@ typedef struct swr_paged {
     int64_t window;            /* 0: all positions; else the last `window` of them         */
     int64_t sq_b, sq_h;        /* strides of q [batch, q_heads, D]                         */
     int64_t sy_b, sy_h;        /* strides of y                                            */
-    float scale;               /* of the products q . k, finite                           */
+    float scale;               /* of the products q . k; finite, also times log2 e         */
     int32_t reserved;          /* must be 0                                               */
 } swr_paged_t;
 

@@ -403,13 +403,16 @@ int swr_cache_append(const swr_cache_t* c, int64_t tokens, const int64_t* sk, co
     return status(swr::launch_append(p, stream));
 }
 
+// Scores are taken times log2 e, in float32.
+static float log2_scale(const swr_paged_t* p) { return p->scale * 1.44269504088896340736f; }
+
 static int resolve_paged(const swr_paged_t* p, int64_t* cache, int64_t* q, int64_t* y) {
     if (!p) return SWR_ERR_NULL;
     const int rc = resolve_cache(&p->cache, cache);
     if (rc != SWR_OK) return rc;
     if (p->batch < 0 || p->q_heads < 1 || p->q_heads % p->cache.heads != 0 || p->max_pages < 0 || p->window < 0)
         return SWR_ERR_SHAPE;
-    if (p->reserved != 0 || !std::isfinite(p->scale) || p->q_heads > 65536 || p->batch > kMaxRows / 65536 ||
+    if (p->reserved != 0 || !std::isfinite(log2_scale(p)) || p->q_heads > 65536 || p->batch > kMaxRows / 65536 ||
         p->max_pages > kMaxWidth)
         return SWR_ERR_UNSUPPORTED;
     const int es = size_of(p->cache.dtype);
@@ -477,7 +480,7 @@ int swr_paged_attention(const swr_paged_t* p, const void* q, const void* k_cache
     a.s_page = (uint32_t)(p->cache.s_page / unit);
     a.s_token = (uint32_t)(p->cache.s_token / unit);
     a.s_head = (uint32_t)(p->cache.s_head / unit);
-    a.scale_log2 = p->scale * 1.44269504088896340736f;
+    a.scale_log2 = log2_scale(p);
     return status(swr::launch_paged(p->cache.dtype, a, stream));
 }
 
