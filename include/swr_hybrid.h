@@ -102,7 +102,8 @@ int64_t swr_rms_norm_workspace_bytes(const swr_norm_t* norm);
  * plus 127 (0 to 252; 255 makes the group NaN; 253 and 254 hold weights beyond
  * float32's range).  Two codes share a byte, the even k in its low half.  A row of codes has ceil(K / 32) groups of 16 bytes, codes past K are
  * not used, and starts 16-byte aligned.  Sums are in float32.  Meant for the
- * few rows of a decoding step (a row of weights is read once for up to 64 rows of x).
+ * few rows of a decoding step (weights are read once for every 32 rows of x; for every 16 of
+ * bf16 rows of 4097 to 8192 elements and of float32 rows of 1025 to 2048).
  * ------------------------------------------------------------------------ */
 
 typedef struct swr_fp4 {

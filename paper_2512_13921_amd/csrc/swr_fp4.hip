@@ -9,16 +9,18 @@
 // their one power:
 //   * bf16 x: the conversion instruction makes bf16 pairs of code times power, exactly;
 //   * 8-bit x: the same against x made bf16, exactly.  (The matrix instruction that takes
-//     codes, powers and 8-bit values as they lie would save the conversions, 33 us for 35
-//     below, but its sums of 128 products are off by up to 1.2e-5 of the sum of their
+//     codes, powers and 8-bit values as they lie would save the conversions, 31.3 us for 32.9
+//     below, and 20 for 28 where x does not stay in registers, 16 x 16384 to 8192; but its sums
+//     of 128 products are off by up to 1.2e-5 of the sum of their
 //     absolute values, which shows in a bf16 y where they cancel);
 //   * float32 x: the same against x split into three bf16 parts, which hold all
 //     of its 24 bits.
 // What bounds it is the weights' bytes, 17 a group of 32: 16 x 8192 8-bit rows
-// against 28672 take 35 us, 3.6 TB/s, where a copy reaches 5.2 and a loop over codes
-// and powers alone 5.0; of it about 7 us are x, which all CUs load first, and 28 us
-// the tiles (4.4 TB/s).  Few or short rows are bound by latency: 2048 to 6176 for one
-// token 4.9 us.  float32 is bound by its conversion and three products.
+// against 28672 take 33 us, 3.8 TB/s, where a copy reaches 5.2 and a loop over codes
+// and powers alone 5.0; against twice as many 61, so that 28 us are the tiles (4.4 TB/s) and 5
+// what is before them, the launch and x, which all CUs load first.  Few or short rows are bound
+// by latency: 2048 to 6176 for one token 4.7 us.  float32 is bound by its conversion, anew for
+// every tile where x does not stay in registers (past 2048), and three products.
 #include <algorithm>
 #include <type_traits>
 
@@ -140,8 +142,8 @@ struct Fragment<XFp8> {
     __device__ u32x4 get(int i) const { return v[i]; }
     static __device__ int at(int i, int q, int g, int G) { return 32 * (q * G + g) + 16 * i; }
     // Hides from the compiler that the values are the last tile's still, as it would convert
-    // them once for all: faster where that fits (64 x 4096 to 4096 9.5 us, 12.2 hidden), and
-    // spilled where not (64 x 8192 to 28672 254 us, 82 hidden).
+    // them once for all: faster where that fits (64 x 4096 to 4096 9.0 us, 9.4 hidden), and
+    // spilled where not (64 x 8192 to 28672 250 us, 69 hidden).
     __device__ void hide() { asm volatile("" : "+v"(v[0]), "+v"(v[1])); }
     __device__ bf16x8 part(int j, int) const {
         const uint32_t lo = v[j / 2][j % 2 * 2], hi = v[j / 2][j % 2 * 2 + 1];
@@ -532,16 +534,20 @@ hipError_t hold(const Fp4Params& p, hipStream_t st) {
 }
 
 // Which kernel, in us (split with one tile of W a wave, with two, held):
-//     rows of x     1000 to 1001     4096 to 4096     8192 to 8192        8192 to 28672
-//     1 bf16        4.5   -   4.2    5.0  6.7  6.3    12.2  13.3  14.4    46  41  36
-//     8 8-bit       4.4   -   4.4    5.1   -   4.8     -    13.3  13.0     -   -  35
-//     16 bf16        -    -    -     8.9  9.0  6.3    24.0  18.9  14.3    102 86  37
-//     5 float32     6.1   -   4.3     (does not fit)
+//     rows of x     2048 to 6176      4096 to 4096      8192 to 4096      8192 to 8192      8192 to 28672
+//     1 bf16        4.6  4.4  4.7     4.6  6.6  6.1     8.1 11.6 10.6    12.4 13.3 14.1     45  39  35
+//     8 bf16        5.9  5.0  4.7     6.2  7.7  6.3    10.1 13.3 10.9    17.7 14.8 14.3     71  60  35
+//     8 8-bit       4.9  4.5  4.6     5.2  6.7  5.4     8.7 11.2  9.2    13.7 13.3 13.2     44  44  33
+//     16 bf16       7.4  5.8  4.8     8.8  9.3  6.4    15.2 17.2 11.3    27.0 19.0 14.2    107  84  35
+//     1 float32     9.4  6.7  6.8     8.8 11.4   -     17.2 21.9   -     31.7 23.9   -     112  93   -
 // The split kernel's lanes load x with a cache line for each of its rows, time after time; the
 // held one's load it once, but before all else, which few rows and few tiles pay back only
 // where x is short, of two blocks of 128 k a wave at most.  It has one block a CU (two: 10 %
 // slower).  Past 16 rows of x it takes 32 at a time if they fit (64 x 4096 to 4096,
-// bf16: 11.2 us, the split kernel 13.7).
+// bf16: 11.0 us, the split kernel 13.5).
+// Two tiles a wave, past 256 of them, serve rows of float32 and several of bf16; they cost one row
+// of 8192 to 8192 7 %, and 8-bit rows that do not fit more: 16384 to 8192, 18.4 us for one row with
+// one tile, 24.9 with two (16 rows: 28.6 and 28.2).
 template <class X, class Y>
 hipError_t by_size(const Fp4Params& p, hipStream_t st) {
     const int tiles = (p.N + 15) / 16;

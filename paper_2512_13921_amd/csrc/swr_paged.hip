@@ -159,23 +159,26 @@ __global__ __launch_bounds__(256) void swr_append_kernel(AppendParams p) {
 // and are joined in LDS.  A row cut between workgroups leaves its parts
 // in the workspace, which swr_paged_join_kernel joins.
 //
-// What bounds it is K and V, read once: 2 requests of 262147 tokens (4 heads of 128 for
-// 32, bf16) 378 to 390 us, 5.5 to 5.7 TB/s, where a copy reaches 5.2; 64 of 17 to 32768 tokens
-// 229 us, 4.9 TB/s, of which 5 are the join.  Short rows are bound by the trips to memory,
-// length, table, K, V: 4 requests of 300 to 700 tokens 11 us.
+// What bounds it is K and V, read once: 2 requests of 262147 tokens (8 heads of 128 for
+// 32, bf16) 391 to 395 us, 5.5 TB/s, where a copy reaches 5.2; 64 of 17 to 32768 tokens
+// 225 to 231 us, 4.9 to 5.0 TB/s, of which 5 are the join.  Short rows are bound by the trips to memory,
+// length, table, K, V: 4 requests of 300 to 700 tokens 12 us.  (With P in two parts, about 17 bits,
+// 256 rows of 900 tokens took 22.9 us where they take 23.6, 2 requests of 262147 1 % less.)
 
 constexpr int kTile = 32;      // tokens of a wave's tile
 constexpr int kWaves = 4;
-// Positions up to which a row is one block's.  (16 rows of 500 tokens, heads of 128, bf16:
-// 9.4 us, 13.2 in shares; of 1000 15.1 and 13.5, of 1500 20.3 and 14.0.  256 rows gain past it
-// if they are alike, 1500 tokens 42 and 50, and lose if not, 17 to 2000 tokens 27.6 and 23.3.)
+// Positions that a table (or a window) may have for its rows to be one block's each; the
+// lengths are not known here.  (16 rows of 500 tokens, heads of 128, bf16:
+// 9.9 us, 13.6 in shares, as they go in a wider table; of 1000 16.0 and 13.8, of 1500 20.7 and
+// 14.2.  256 rows gain past it
+// if they are alike, 1500 tokens 41 and 50, and lose if not, 17 to 2000 tokens 27.7 and 23.6.)
 constexpr int kShort = 1024;
 constexpr int64_t kMostRows = 1 << 23;   // (a launch has fewer than 2^32 threads, a row 512 of them)
 // Shares of the work: three workgroups a compute unit, which is what a unit
 // holds of heads of up to 256 bytes.  Not a power of two: of equal rows, whose
 // lengths mostly are, shares would begin at multiples of large powers of two and so
 // on few of the memory's channels (2 requests of 262147 tokens, 16 heads of 64, bf16: 512
-// shares 492 us, 768 410, 1024 482; 8 heads of 128: 408, 374, 398).
+// shares 476 us, 768 419, 1024 416; 8 heads of 128: 425, 396, 419).
 constexpr int kShares = 768;
 constexpr int kRowCost = 4;
 
@@ -194,8 +197,8 @@ __device__ inline Rows rows_of(const PagedParams& p, int b) {
 // The flat order: (request, head row within the request, place within the row).
 // A row takes kRowCost places, in which nothing is done, before its tiles: what
 // beginning and joining a row costs, in tiles, so that shares of many short rows are
-// no longer than others (100 requests of 10 to 5000 tokens, 4 rows each: 45.0 us, with
-// 0 places 59.6).
+// no longer than others (100 requests of 10 to 5000 tokens, 4 rows each: 45.3 us, with
+// 0 places 61.8).
 struct Place {
     int64_t total;   // places of all rows
     int64_t per;     // places a workgroup
@@ -654,8 +657,8 @@ __global__ __launch_bounds__(kWaves * 64, waves_held(DP * sizeof(typename E::T))
 
 // Rows of few tokens, each a block's of its own: no shares to find or to join.
 // Eight waves, or four of heads past 128 channels, for their registers (256 rows of 900
-// tokens: 256 channels of float32 209 us with eight, 106 with four, of bf16 52.6 and
-// 49.7; 128 of float32 52.3 and 57.3).
+// tokens: 256 channels of float32 209 us with eight, 106 with four, of bf16 52.9 and
+// 51.0, though 16 rows of 500 take 16.2 and 17.8; 128 of float32 52 and 57).
 constexpr int short_waves(int channels) { return channels > 128 ? 4 : 8; }
 
 template <class E, int DP, bool FULL>
@@ -689,7 +692,7 @@ struct Sum {
 };
 
 // Few rows are found by a block each, many by the shares that they begin in (4 rows of
-// 100000 tokens: 54.9 us, by shares 57.9; 800 of 1100 to 3000: 169.0, by shares 163.5).
+// 100000 tokens: 55.1 us, by shares 58.2; 800 of 1100 to 3000: 169.2, by shares 164.9).
 __host__ __device__ inline bool by_row(int rows, int shares) { return rows < shares / 4; }
 
 template <class E, int DP>
@@ -760,7 +763,7 @@ hipError_t go(const PagedParams& p, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     // Two teams where a row has a few parts on average, up to eight where it has many (800
-    // rows of 1100 to 3000 tokens 163.5 us, with eight 173.7; 4 rows of 100000 54.9, with two 61.0).
+    // rows of 1100 to 3000 tokens 164.9 us, with eight 173.5; 4 rows of 100000 55.1, with two 61.6).
     const int rows = p.batch * p.kv_heads * p.head_tiles, shares = p.workgroups;
     const int teams = rows >= shares / 8 ? 2 : rows >= shares / 64 ? 4 : 8;
     const int slices = std::min((std::min(p.group, 16) * DP + 127) / 128, by_row(rows, shares) ? 32 : 4);

@@ -60,7 +60,7 @@ def test_linear(swr, dtype, M, N, K):
         _check(swr, x, codes, powers, scale, out)
 
 
-# Each way through the kernels: x held in registers of every length (one to sixteen blocks
+# Each way through the kernels: x held in registers of every length (one to eight blocks
 # of 128 k a wave), 16 and 32 rows at a time; several meetings of a workgroup's waves, the
 # last one short; x that does not fit; one tile of W a wave and two.
 LONG = [(9, 40, 1100), (12, 50, 3000), (16, 33, 4097), (10, 50, 6000), (16, 40, 8191), (11, 48, 16384), (10, 33, 16390),
