@@ -74,7 +74,10 @@ def test_missing_pages(swr):
     table[0, 3], table[0, 7], table[1, 0], table[3, 0] = -1, kc.shape[0], 2 ** 31 - 1, -2 ** 31
     table[0, 40:60], table[1, 1:20], table[4] = -1, -5, -1       # whole tiles, and a whole request
     _check(swr, _q(8, 5, 4, 64, BF16), kc, vc, table, n)
-    _check(swr, _q(8, 5, 4, 64, BF16), kc, vc, table, _i32([5000, 500, 2 ** 31 - 1, 10, 1300]))
+    # lengths past the table's columns end with it
+    q, end = _q(8, 5, 4, 64, BF16), 16 * table.shape[1]
+    want = _check(swr, q, kc, vc, table, _i32([end, 500, end, 10, 1300]))
+    assert torch.equal(swr.swr_paged_attention(q, kc, vc, table, _i32([5000, 500, 2 ** 31 - 1, 10, 1300])), want)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
