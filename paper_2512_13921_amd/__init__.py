@@ -35,7 +35,11 @@ __all__ = ["SwrError", "swr_forward", "swr_backward", "swr_carriers", "swr_error
            "swr_forward_shared_gates", "swr_backward_shared_gates", "swr_shared_gates_workspace_bytes",
            "SWRFunction", "SWRUniformFunction", "SWRSharedGatesFunction", "library_path", "load",
            "swr_rms_norm", "swr_rms_norm_backward", "swr_fp4_pack", "swr_fp4_linear", "swr_block_tables",
-           "swr_cache_append", "swr_paged_attention", "SWRNormFunction"]
+           "swr_cache_append", "swr_paged_attention", "SWRNormFunction",
+           "swr_embedding", "swr_embedding_backward", "swr_causal_conv", "swr_causal_conv_step",
+           "swr_causal_conv_backward", "swr_selective_scan", "swr_selective_step", "swr_selective_scan_backward",
+           "swr_log_probs", "swr_log_probs_backward", "SWREmbeddingFunction", "SWRCausalConvFunction",
+           "SWRSelectiveScanFunction", "SWRLogProbsFunction"]
 
 SWR_ABI_VERSION = 1
 SWR_DTYPE_F32 = 0
@@ -868,9 +872,15 @@ def __getattr__(name):
         return _FUNCTIONS[name]
     if name == "SWRNormFunction":
         return hybrid.SWRNormFunction
+    if name in ("SWREmbeddingFunction", "SWRCausalConvFunction", "SWRSelectiveScanFunction", "SWRLogProbsFunction"):
+        return getattr(lm, name)
     raise AttributeError(name)
 
 
 from . import hybrid  # noqa: E402  (it marshals with the functions above)
 from .hybrid import (swr_block_tables, swr_cache_append, swr_fp4_linear, swr_fp4_pack,  # noqa: E402
                      swr_paged_attention, swr_rms_norm, swr_rms_norm_backward)
+from . import lm  # noqa: E402
+from .lm import (swr_causal_conv, swr_causal_conv_backward, swr_causal_conv_step, swr_embedding,  # noqa: E402
+                 swr_embedding_backward, swr_log_probs, swr_log_probs_backward, swr_selective_scan,
+                 swr_selective_scan_backward, swr_selective_step)

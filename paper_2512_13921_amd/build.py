@@ -19,11 +19,15 @@ BINDING = os.path.join(HERE, "_binding.so")
 BINDING_SOURCE = os.path.join(CSRC, "swr_binding.cpp")
 ABI_HEADER = os.path.join(os.path.dirname(HERE), "include", "swr.h")
 HYBRID_HEADER = os.path.join(os.path.dirname(HERE), "include", "swr_hybrid.h")
+LM_HEADER = os.path.join(os.path.dirname(HERE), "include", "swr_lm.h")
 SOURCES = [os.path.join(CSRC, n) for n in ("swr_api.cpp", "swr_kernels.hip", "swr_uniform.hip", "swr_groups.hip",
                                             "swr_noalloc.hip", "swr_chain.hip", "swr_hybrid_api.cpp", "swr_norm.hip",
-                                            "swr_fp4.hip", "swr_paged.hip")]
+                                            "swr_fp4.hip", "swr_paged.hip", "swr_lm_api.cpp", "swr_embed.hip",
+                                            "swr_conv.hip", "swr_scan.hip", "swr_logprob.hip")]
 HEADERS = [os.path.join(CSRC, "swr_launch.h"), os.path.join(CSRC, "swr_device.h"),
-           os.path.join(CSRC, "swr_internal.h"), os.path.join(CSRC, "swr_hybrid_launch.h"), ABI_HEADER, HYBRID_HEADER]
+           os.path.join(CSRC, "swr_internal.h"), os.path.join(CSRC, "swr_hybrid_launch.h"),
+           os.path.join(CSRC, "swr_lm_launch.h"), os.path.join(CSRC, "swr_vectors.h"), os.path.join(CSRC, "swr_checks.h"),
+           ABI_HEADER, HYBRID_HEADER, LM_HEADER]
 ARCH = "gfx950"
 
 
@@ -93,7 +97,7 @@ def binding_key() -> str:
     and the Python and torch that it is compiled against."""
     import torch
     key = hashlib.sha256(f"{sys.version} {torch.__version__}".encode())
-    for path in (BINDING_SOURCE, ABI_HEADER, HYBRID_HEADER):
+    for path in (BINDING_SOURCE, ABI_HEADER, HYBRID_HEADER, LM_HEADER):
         with open(path, "rb") as f:
             key.update(f.read())
     return key.hexdigest()

@@ -18,8 +18,11 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
+
 #include "../../include/swr.h"
 #include "../../include/swr_hybrid.h"
+#include "../../include/swr_lm.h"
 
 // What this module was built from and for; the build looks for it in the file.
 extern "C" __attribute__((used)) const char swr_binding_key[] = "swr-binding-key:" SWR_BINDING_KEY;
@@ -64,6 +67,28 @@ union {
     HybridAbi fn;
     void* address[kHybridEntries];
 } hybrid;
+
+// Those of a recurrent language model's.
+struct LmAbi {
+    decltype(&swr_embedding) embedding;
+    decltype(&swr_embedding_workspace_bytes) embedding_workspace_bytes;
+    decltype(&swr_embedding_backward) embedding_backward;
+    decltype(&swr_causal_conv) causal_conv;
+    decltype(&swr_causal_conv_workspace_bytes) causal_conv_workspace_bytes;
+    decltype(&swr_causal_conv_backward) causal_conv_backward;
+    decltype(&swr_selective_scan) selective_scan;
+    decltype(&swr_selective_scan_workspace_bytes) selective_scan_workspace_bytes;
+    decltype(&swr_selective_scan_backward) selective_scan_backward;
+    decltype(&swr_selective_scan_backward_workspace_bytes) selective_scan_backward_workspace_bytes;
+    decltype(&swr_log_probs) log_probs;
+    decltype(&swr_log_probs_workspace_bytes) log_probs_workspace_bytes;
+    decltype(&swr_log_probs_backward) log_probs_backward;
+};
+constexpr int kLmEntries = sizeof(LmAbi) / sizeof(void*);
+union {
+    LmAbi fn;
+    void* address[kLmEntries];
+} language;
 
 // Arguments of one call, taken in order; ok turns false at the first that is
 // not what the fast path handles.
@@ -672,6 +697,407 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---------------------------------------------------------------------------
+// A recurrent language model's operators
+// ---------------------------------------------------------------------------
+
+// Tokens of a shape, int32 or int64: a token's bytes, or 0.
+int token_bytes(const at::Tensor& t, const at::Tensor& x, at::IntArrayRef shape) {
+    const bool wide = t.scalar_type() == at::kLong;
+    return (wide || t.scalar_type() == at::kInt) && dense(t, x, t.scalar_type(), shape) ? wide ? 8 : 4 : 0;
+}
+// Rows of t, equally spaced: their stride.
+bool even_rows(const at::Tensor& t, int64_t* n, int64_t* stride) {
+    int64_t outer, inner, so, si;
+    if (!rows(t, &outer, &inner, &so, &si) || (outer > 1 && inner > 1 && so != inner * si)) return false;
+    *n = outer * inner;
+    *stride = inner > 1 ? si : so;
+    return true;
+}
+
+// embedding(tokens, table, scale, stream) -> y
+PyObject* embedding(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    const at::Tensor &tokens = g.tensor(), &table = g.tensor();
+    swr_embed_t e = {};
+    e.scale = (float)g.real();
+    if (!g.ok || !std::isfinite(e.scale) || !table.is_cuda() || !float_or_bf16(table) || !matrix(table)) return none();
+    void* st = stream_of(*g.v, table, &g.ok);
+    e.token_bytes = token_bytes(tokens, table, tokens.sizes());
+    if (!g.ok || !e.token_bytes) return none();
+    e.abi_version = SWR_ABI_VERSION;
+    e.dtype = e.out_dtype = code_of(table);
+    e.tokens = tokens.numel(); e.vocab = table.size(0); e.width = table.size(1);
+    e.st = table.stride(0); e.sy = e.width;
+    at::Tensor y;
+    int rc;
+    {
+        const Unlocked unlocked;
+        auto shape = tokens.sizes().vec();
+        shape.push_back(e.width);
+        y = made(table, shape, table.scalar_type());
+        rc = language.fn.embedding(&e, ptr(tokens), ptr(table), ptr(y), st);
+    }
+    return results(rc, {y});
+    END_HANDLE_TH_ERRORS
+}
+
+// embedding_backward(tokens, dy, vocab, scale, in_dtype, stream) -> dtable
+PyObject* embedding_backward(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    const at::Tensor &tokens = g.tensor(), &dy = g.tensor();
+    swr_embed_t e = {};
+    e.vocab = g.integer();
+    e.scale = (float)g.real();
+    const bool same = g.truth();
+    int64_t n;
+    if (!g.ok || !std::isfinite(e.scale) || !dy.is_cuda() || !float_or_bf16(dy) || !even_rows(dy, &n, &e.sy) || e.vocab < 1)
+        return none();
+    void* st = stream_of(*g.v, dy, &g.ok);
+    e.token_bytes = token_bytes(tokens, dy, dy.sizes().slice(0, dy.dim() - 1));
+    if (!g.ok || !e.token_bytes) return none();
+    e.abi_version = SWR_ABI_VERSION;
+    e.dtype = code_of(dy);
+    e.out_dtype = same ? e.dtype : SWR_DTYPE_F32;
+    e.tokens = n; e.width = dy.size(-1);
+    e.st = e.width;
+    const int64_t ws = language.fn.embedding_workspace_bytes(&e);
+    if (ws < 0) return none();
+    const at::Tensor work = workspace(dy, std::max<int64_t>(ws / 4, 4), *g.v, st);
+    at::Tensor d;
+    int rc;
+    {
+        const Unlocked unlocked;
+        d = made(dy, {e.vocab, e.width}, same ? dy.scalar_type() : at::kFloat);
+        rc = language.fn.embedding_backward(&e, ptr(tokens), ptr(dy), ptr(d), ptr(work), st);
+    }
+    return results(rc, {d});
+    END_HANDLE_TH_ERRORS
+}
+
+bool conv_problem(const at::Tensor& x, const at::Tensor& w, const at::Tensor& bias, bool silu, swr_conv_t* p) {
+    *p = swr_conv_t{};
+    const int64_t d = x.dim();
+    if (!x.is_cuda() || !float_or_bf16(x) || d < 2 || d > 3 || w.dim() != 2 || (x.stride(d - 1) != 1 && x.size(d - 1) > 1))
+        return false;
+    p->abi_version = SWR_ABI_VERSION;
+    p->dtype = code_of(x);
+    p->flags = silu ? SWR_CONV_SILU : 0;
+    p->taps = (int32_t)std::min<int64_t>(w.size(1), 9);   // (more are refused)
+    p->B = x.size(0); p->T = d == 3 ? x.size(1) : 1; p->C = x.size(d - 1);
+    p->sx_b = x.stride(0); p->sx_t = d == 3 ? x.stride(1) : 0;
+    p->sy_b = p->sd_b = p->T * p->C; p->sy_t = p->sd_t = p->C;
+    return dense(w, x, x.scalar_type(), {p->C, w.size(1)}) && (!bias.defined() || dense(bias, x, x.scalar_type(), {p->C}));
+}
+bool lengths_of(const at::Tensor& n, const at::Tensor& x) { return !n.defined() || dense(n, x, at::kInt, {x.size(0)}); }
+
+// causal_conv(x, weight, bias, silu, state, lengths, want_state, stream) -> (y, state)
+PyObject* causal_conv(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    const at::Tensor &x = g.tensor(), &w = g.tensor();
+    const at::Tensor bias = g.optional();
+    const bool silu = g.truth();
+    const at::Tensor state = g.optional(), lengths = g.optional();
+    const bool want = g.truth();
+    swr_conv_t p;
+    if (!g.ok || x.dim() != 3 || !conv_problem(x, w, bias, silu, &p) || !lengths_of(lengths, x)) return none();
+    void* st = stream_of(*g.v, x, &g.ok);
+    const std::array<int64_t, 3> shape{p.B, p.taps - 1, p.C};
+    if (!g.ok || (state.defined() && !dense(state, x, x.scalar_type(), shape))) return none();
+    at::Tensor y, s;
+    int rc;
+    {
+        const Unlocked unlocked;
+        y = made(x, x.sizes(), x.scalar_type());
+        if (want) s = made(x, shape, x.scalar_type());
+        rc = language.fn.causal_conv(&p, ptr(x), ptr(w), ptr(bias), ptr(state), (const int32_t*)ptr(lengths), ptr(y),
+                                     ptr(s), st);
+    }
+    return results(rc, {y, s});
+    END_HANDLE_TH_ERRORS
+}
+
+// causal_conv_step(x, weight, state, bias, silu, stream) -> y
+PyObject* causal_conv_step(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    const at::Tensor &x = g.tensor(), &w = g.tensor(), &state = g.tensor();
+    const at::Tensor bias = g.optional();
+    const bool silu = g.truth();
+    swr_conv_t p;
+    if (!g.ok || x.dim() != 2 || !conv_problem(x, w, bias, silu, &p)) return none();
+    void* st = stream_of(*g.v, x, &g.ok);
+    if (!g.ok || !dense(state, x, x.scalar_type(), {p.B, p.taps - 1, p.C})) return none();
+    at::Tensor y;
+    int rc;
+    {
+        const Unlocked unlocked;
+        y = made(x, x.sizes(), x.scalar_type());
+        rc = language.fn.causal_conv(&p, ptr(x), ptr(w), ptr(bias), ptr(state), nullptr, ptr(y), ptr(state), st);
+    }
+    return results(rc, {y});
+    END_HANDLE_TH_ERRORS
+}
+
+// causal_conv_backward(x, weight, dy, bias, silu, lengths, stream) -> (dx, dweight, dbias)
+PyObject* causal_conv_backward(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    const at::Tensor &x = g.tensor(), &w = g.tensor(), &dy = g.tensor();
+    const at::Tensor bias = g.optional();
+    const bool silu = g.truth();
+    const at::Tensor lengths = g.optional();
+    swr_conv_t p;
+    if (!g.ok || x.dim() != 3 || !conv_problem(x, w, bias, silu, &p) || !lengths_of(lengths, x) ||
+        !is(dy, x, x.scalar_type(), x.sizes()) || (dy.stride(2) != 1 && p.C > 1))
+        return none();
+    p.sy_b = dy.stride(0); p.sy_t = dy.stride(1);
+    void* st = stream_of(*g.v, x, &g.ok);
+    if (!g.ok) return none();
+    const int64_t ws = language.fn.causal_conv_workspace_bytes(&p);
+    if (ws < 0) return none();
+    const at::Tensor work = workspace(x, std::max<int64_t>(ws / 4, 4), *g.v, st);
+    at::Tensor dx, dw, db;
+    int rc;
+    {
+        const Unlocked unlocked;
+        dx = made(x, x.sizes(), x.scalar_type());
+        dw = made(x, w.sizes(), at::kFloat);
+        if (bias.defined()) db = made(x, bias.sizes(), at::kFloat);
+        rc = language.fn.causal_conv_backward(&p, ptr(x), ptr(w), ptr(bias), ptr(dy), (const int32_t*)ptr(lengths),
+                                              ptr(dx), fptr(dw), fptr(db), ptr(work), st);
+    }
+    return results(rc, {dx, dw, db});
+    END_HANDLE_TH_ERRORS
+}
+
+// The scan's inputs as its calls have them, first of all: x, dt, A, B, C.
+struct ScanArgs {
+    const at::Tensor &x, &dt, &A, &B, &C;
+    at::Tensor D, z, bias, h0, lengths;
+    swr_scan_t p = {};
+    swr_scan_inputs_t in = {};
+    explicit ScanArgs(Args& g) : x(g.tensor()), dt(g.tensor()), A(g.tensor()), B(g.tensor()), C(g.tensor()) {}
+
+    // [B, T, n] (or [B, n]) of x's type: its strides.
+    bool sequence(const at::Tensor& t, int64_t* sb, int64_t* s_t) const {
+        const int64_t d = x.dim();
+        if (!is(t, x, x.scalar_type(), x.sizes()) || (t.stride(d - 1) != 1 && t.size(d - 1) > 1)) return false;
+        *sb = t.stride(0);
+        *s_t = d == 3 ? t.stride(1) : 0;
+        return true;
+    }
+    bool shared(const at::Tensor& t, int64_t* sb, int64_t* s_t, int64_t* sg) const {
+        const int64_t d = t.dim(), lead = x.dim() - 1;
+        const bool groups = B.dim() == x.dim() + 1;
+        if (t.scalar_type() != x.scalar_type() || t.device() != x.device() || t.sizes() != B.sizes() ||
+            t.sizes().slice(0, lead) != x.sizes().slice(0, lead) || t.size(d - 1) != p.N ||
+            (t.stride(d - 1) != 1 && p.N > 1))
+            return false;
+        *sb = t.stride(0);
+        *s_t = lead == 2 ? t.stride(1) : 0;
+        *sg = groups ? t.stride(d - 2) : 0;
+        return true;
+    }
+    bool check(const Args& g, bool softplus) {
+        const int64_t d = x.dim();
+        if (!g.ok || !x.is_cuda() || !float_or_bf16(x) || d < 2 || d > 3 || A.dim() != 2 ||
+            (B.dim() != d && B.dim() != d + 1))
+            return false;
+        p.abi_version = SWR_ABI_VERSION;
+        p.dtype = code_of(x);
+        p.flags = softplus ? SWR_SCAN_SOFTPLUS : 0;
+        p.N = (int32_t)std::min<int64_t>(A.size(1), 65);   // (more are refused)
+        p.B = x.size(0); p.T = d == 3 ? x.size(1) : 1; p.D = x.size(d - 1);
+        p.G = B.dim() == d + 1 ? B.size(d - 1) : 1;
+        if (A.size(1) != p.N || p.G < 1 || p.D % p.G != 0) return false;
+        p.sy_b = p.T * p.D; p.sy_t = p.D;
+        const auto channel = [&](const at::Tensor& t) { return !t.defined() || dense(t, x, at::kFloat, {p.D}); };
+        if (!dense(A, x, at::kFloat, {p.D, p.N}) || !sequence(x, &p.sx_b, &p.sx_t) || !sequence(dt, &p.sdt_b, &p.sdt_t) ||
+            (z.defined() && !sequence(z, &p.sz_b, &p.sz_t)) || !shared(B, &p.sB_b, &p.sB_t, &p.sB_g) ||
+            !shared(C, &p.sC_b, &p.sC_t, &p.sC_g) || !channel(D) || !channel(bias) ||
+            (h0.defined() && !dense(h0, x, at::kFloat, {p.B, p.D, p.N})) || !lengths_of(lengths, x))
+            return false;
+        in = {ptr(x), ptr(dt), fptr(A), ptr(B), ptr(C), fptr(bias), fptr(D), ptr(z), fptr(h0), (const int32_t*)ptr(lengths)};
+        return true;
+    }
+};
+
+// selective_scan(x, dt, A, B, C, D, z, dt_bias, softplus, h0, lengths, save_carriers, want_state, stream)
+//     -> (y, carriers, h_last)
+PyObject* selective_scan(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    ScanArgs a(g);
+    a.D = g.optional(); a.z = g.optional(); a.bias = g.optional();
+    const bool softplus = g.truth();
+    a.h0 = g.optional(); a.lengths = g.optional();
+    const bool save = g.truth(), want = g.truth();
+    if (!a.check(g, softplus) || a.x.dim() != 3) return none();
+    void* st = stream_of(*g.v, a.x, &g.ok);
+    if (!g.ok) return none();
+    const int64_t ws = language.fn.selective_scan_workspace_bytes(&a.p);
+    if (ws < 0) return none();
+    at::Tensor work, y, carriers, h;
+    if (ws > 0) work = workspace(a.x, ws / 4, *g.v, st);
+    int rc;
+    {
+        const Unlocked unlocked;
+        y = made(a.x, a.x.sizes(), a.x.scalar_type());
+        if (save)
+            carriers = made(a.x, {a.p.B, (a.p.T + SWR_SCAN_BLOCK - 1) / SWR_SCAN_BLOCK, a.p.D, a.p.N}, at::kFloat);
+        if (want) h = made(a.x, {a.p.B, a.p.D, a.p.N}, at::kFloat);
+        rc = language.fn.selective_scan(&a.p, &a.in, ptr(y), fptr(carriers), fptr(h), ptr(work), st);
+    }
+    return results(rc, {y, carriers, h});
+    END_HANDLE_TH_ERRORS
+}
+
+// selective_step(x, dt, A, B, C, state, D, z, dt_bias, softplus, stream) -> y
+PyObject* selective_step(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    ScanArgs a(g);
+    a.h0 = g.tensor();
+    a.D = g.optional(); a.z = g.optional(); a.bias = g.optional();
+    const bool softplus = g.truth();
+    if (!a.check(g, softplus) || a.x.dim() != 2) return none();
+    void* st = stream_of(*g.v, a.x, &g.ok);
+    if (!g.ok) return none();
+    const int64_t ws = language.fn.selective_scan_workspace_bytes(&a.p);
+    if (ws != 0) return none();   // (a token needs none)
+    at::Tensor y;
+    int rc;
+    {
+        const Unlocked unlocked;
+        y = made(a.x, a.x.sizes(), a.x.scalar_type());
+        rc = language.fn.selective_scan(&a.p, &a.in, ptr(y), nullptr, fptr(a.h0), nullptr, st);
+    }
+    return results(rc, {y});
+    END_HANDLE_TH_ERRORS
+}
+
+// selective_scan_backward(x, dt, A, B, C, dy, carriers, D, z, dt_bias, softplus, dh_last, lengths, want_dh0, stream)
+//     -> (dx, ddt, dA, dB, dC, dD, dz, ddt_bias, dh0)
+PyObject* selective_scan_backward(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    ScanArgs a(g);
+    const at::Tensor &dy = g.tensor(), &carriers = g.tensor();
+    a.D = g.optional(); a.z = g.optional(); a.bias = g.optional();
+    const bool softplus = g.truth();
+    const at::Tensor dh = g.optional();
+    a.lengths = g.optional();
+    const bool want = g.truth();
+    if (!a.check(g, softplus) || a.x.dim() != 3 || !a.sequence(dy, &a.p.sy_b, &a.p.sy_t)) return none();
+    void* st = stream_of(*g.v, a.x, &g.ok);
+    const std::array<int64_t, 3> hs{a.p.B, a.p.D, a.p.N};
+    if (!g.ok || (dh.defined() && !dense(dh, a.x, at::kFloat, hs)) ||
+        !dense(carriers, a.x, at::kFloat, {a.p.B, (a.p.T + SWR_SCAN_BLOCK - 1) / SWR_SCAN_BLOCK, a.p.D, a.p.N}))
+        return none();
+    const int64_t ws = language.fn.selective_scan_backward_workspace_bytes(&a.p);
+    if (ws < 0) return none();
+    const at::Tensor work = workspace(a.x, std::max<int64_t>(ws / 4, 4), *g.v, st);
+    at::Tensor dx, ddt, dA, dB, dC, dD, dz, db, dh0;
+    int rc;
+    {
+        const Unlocked unlocked;
+        const auto dense_like = [&](const at::Tensor& t) { return made(a.x, t.sizes(), t.scalar_type()); };
+        dx = dense_like(a.x);
+        ddt = dense_like(a.dt);
+        dA = dense_like(a.A);
+        dB = dense_like(a.B);
+        dC = dense_like(a.C);
+        if (a.D.defined()) dD = dense_like(a.D);
+        if (a.z.defined()) dz = dense_like(a.z);
+        if (a.bias.defined()) db = dense_like(a.bias);
+        if (want) dh0 = made(a.x, hs, at::kFloat);
+        const swr_scan_gradients_t out{ptr(dx), ptr(ddt), fptr(dA), ptr(dB), ptr(dC), fptr(db), fptr(dD), ptr(dz), fptr(dh0)};
+        rc = language.fn.selective_scan_backward(&a.p, &a.in, ptr(dy), fptr(carriers), fptr(dh), &out, ptr(work), st);
+    }
+    return results(rc, {dx, ddt, dA, dB, dC, dD, dz, db, dh0});
+    END_HANDLE_TH_ERRORS
+}
+
+bool logprob_problem(const at::Tensor& x, const at::Tensor& tokens, double scale, swr_logprob_t* p) {
+    *p = swr_logprob_t{};
+    if (!x.is_cuda() || !float_or_bf16(x) || !even_rows(x, &p->rows, &p->sl)) return false;
+    p->token_bytes = token_bytes(tokens, x, x.sizes().slice(0, x.dim() - 1));
+    if (!p->token_bytes || !std::isfinite(scale)) return false;
+    p->abi_version = SWR_ABI_VERSION;
+    p->dtype = code_of(x);
+    p->vocab = x.size(-1);
+    p->sd = p->vocab;
+    p->scale = (float)scale;
+    return true;
+}
+
+// log_probs(logits, tokens, top, scale, stream) -> (logp, lse, entropy, top_logp, top_tokens)
+PyObject* log_probs(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    const at::Tensor &x = g.tensor(), &tokens = g.tensor();
+    const int64_t top = g.integer();
+    const double scale = g.real();
+    swr_logprob_t p;
+    if (!g.ok || !logprob_problem(x, tokens, scale, &p) || top < 0 || top > std::min<int64_t>(p.vocab, SWR_TOP_MOST))
+        return none();
+    p.top = (int32_t)top;
+    void* st = stream_of(*g.v, x, &g.ok);
+    if (!g.ok) return none();
+    const int64_t ws = language.fn.log_probs_workspace_bytes(&p);
+    if (ws < 0) return none();
+    at::Tensor work, logp, lse, entropy, best, at;
+    if (ws > 0) work = workspace(x, (ws + 3) / 4, *g.v, st);
+    int rc;
+    {
+        const Unlocked unlocked;
+        const auto lead = x.sizes().slice(0, x.dim() - 1);
+        logp = made(x, lead, at::kFloat);
+        lse = made(x, lead, at::kFloat);
+        entropy = made(x, lead, at::kFloat);
+        if (top) {
+            auto shape = lead.vec();
+            shape.push_back(top);
+            best = made(x, shape, at::kFloat);
+            at = made(x, shape, at::kLong);
+        }
+        rc = language.fn.log_probs(&p, ptr(x), ptr(tokens), fptr(logp), fptr(lse), fptr(entropy), fptr(best),
+                                   (int64_t*)ptr(at), ptr(work), st);
+    }
+    return results(rc, {logp, lse, entropy, best, at});
+    END_HANDLE_TH_ERRORS
+}
+
+// log_probs_backward(logits, tokens, lse, entropy, dlogp, dentropy, dlse, scale, stream) -> dlogits
+PyObject* log_probs_backward(PyObject*, PyObject* const* v, Py_ssize_t) {
+    HANDLE_TH_ERRORS
+    Args g{v};
+    const at::Tensor &x = g.tensor(), &tokens = g.tensor(), &lse = g.tensor(), &entropy = g.tensor();
+    const at::Tensor dlogp = g.optional(), dentropy = g.optional(), dlse = g.optional();
+    const double scale = g.real();
+    swr_logprob_t p;
+    if (!g.ok || !logprob_problem(x, tokens, scale, &p)) return none();
+    void* st = stream_of(*g.v, x, &g.ok);
+    const auto row = [&](const at::Tensor& t) {
+        return !t.defined() || dense(t, x, at::kFloat, x.sizes().slice(0, x.dim() - 1));
+    };
+    if (!g.ok || !row(lse) || !row(entropy) || !row(dlogp) || !row(dentropy) || !row(dlse)) return none();
+    at::Tensor d;
+    int rc;
+    {
+        const Unlocked unlocked;
+        d = made(x, x.sizes(), x.scalar_type());
+        rc = language.fn.log_probs_backward(&p, ptr(x), ptr(tokens), fptr(lse), fptr(entropy), fptr(dlogp), fptr(dlse),
+                                            fptr(dentropy), ptr(d), st);
+    }
+    return results(rc, {d});
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(address, ...): the C ABI's entry points, in Abi's order
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
     if (n != kEntries) {
@@ -694,12 +1120,26 @@ PyObject* bind_hybrid(PyObject*, PyObject* const* v, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+// bind_lm(address, ...): those of a recurrent language model's, in LmAbi's order
+PyObject* bind_lm(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    if (n != kLmEntries) {
+        PyErr_SetString(PyExc_TypeError, "bind_lm: wrong number of entry points");
+        return nullptr;
+    }
+    for (int i = 0; i < kLmEntries; ++i) language.address[i] = PyLong_AsVoidPtr(v[i]);
+    if (PyErr_Occurred()) return nullptr;
+    Py_RETURN_NONE;
+}
+
 #define ENTRY(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(bind), ENTRY(forward), ENTRY(backward), ENTRY(exact_forward), ENTRY(exact_backward),
                          ENTRY(step), ENTRY(decode_state), ENTRY(uniform_forward), ENTRY(uniform_backward),
                          ENTRY(forward_shared_gates), ENTRY(backward_shared_gates), ENTRY(bind_hybrid),
                          ENTRY(rms_norm), ENTRY(rms_norm_backward), ENTRY(fp4_linear), ENTRY(block_tables),
-                         ENTRY(cache_append), ENTRY(paged_attention), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(cache_append), ENTRY(paged_attention), ENTRY(bind_lm), ENTRY(embedding),
+                         ENTRY(embedding_backward), ENTRY(causal_conv), ENTRY(causal_conv_step),
+                         ENTRY(causal_conv_backward), ENTRY(selective_scan), ENTRY(selective_step),
+                         ENTRY(selective_scan_backward), ENTRY(log_probs), ENTRY(log_probs_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
