@@ -159,7 +159,7 @@ typedef struct swr_scan_inputs {
     const int32_t* lengths;
 } swr_scan_inputs_t;
 
-/* Forward.  y may be NULL where only states are wanted; carriers and h_last (float32 [B, D, N];
+/* Forward.  carriers and h_last (float32 [B, D, N];
  * it may be h0 itself, updated in place) may be NULL. */
 int swr_selective_scan(const swr_scan_t* p, const swr_scan_inputs_t* in, void* y, float* carriers, float* h_last,
                        void* workspace, void* stream);

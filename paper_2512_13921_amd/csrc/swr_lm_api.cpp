@@ -294,12 +294,13 @@ int swr_selective_scan(const swr_scan_t* p, const swr_scan_inputs_t* in, void* y
                        void* workspace, void* stream) {
     if (!in) return SWR_ERR_NULL;
     ScanSizes s;
-    const int rc = resolve(p, in->z != nullptr, !y, &s);
+    const int rc = resolve(p, in->z != nullptr, false, &s);
     if (rc != SWR_OK) return rc;
     if (p->B == 0 || (p->T == 0 && !h_last)) return SWR_OK;
     const swr::ScanPlan plan = swr::plan_scan(*p, false);
     const int64_t work = swr::scan_work_floats(*p, plan) * 4;
-    if (!in->A || (p->T > 0 && (!in->x || !in->dt || !in->B || !in->C)) || (work > 0 && !workspace)) return SWR_ERR_NULL;
+    if (!in->A || (p->T > 0 && (!in->x || !in->dt || !in->B || !in->C || !y)) || (work > 0 && !workspace))
+        return SWR_ERR_NULL;
     if (!all_aligned({in->x, in->dt, in->B, in->C, in->z, y}, s.es) ||
         !all_aligned({in->A, in->bias, in->skip, in->h0, in->lengths, carriers, h_last}, 4) || !aligned(workspace, 16))
         return SWR_ERR_ALIGN;

@@ -39,7 +39,7 @@ hipError_t launch_conv_backward(int dtype, int taps, const ConvParams& p, void* 
 
 // Channels of a block of threads, and runs of tokens that the work is cut into.
 struct ScanPlan {
-    bool wide;                           // 16 states a lane, else 4
+    int states;                          // of a channel, a lane: 4 or 1
     int lanes;                           // lanes that share a channel's states: a power of two
     int64_t chunk;                       // tokens of a run, a multiple of SWR_SCAN_BLOCK
     int64_t chunks;                      // runs of a sequence

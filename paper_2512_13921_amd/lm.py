@@ -14,7 +14,7 @@ import math
 
 import paper_2512_13921_amd as _package
 
-from . import (SWR_ABI_VERSION, SWR_DTYPE_BF16, SWR_DTYPE_F32, _checked, _opt, _ptr, _raw, _stream, _torch, load)
+from . import (SWR_ABI_VERSION, SWR_DTYPE_BF16, SWR_DTYPE_F32, _checked, _on, _opt, _ptr, _raw, _stream, _torch, load)
 from .hybrid import _check, _code, _gpu, _like, _rows, _workspace
 
 __all__ = ["swr_embedding", "swr_embedding_backward", "swr_causal_conv", "swr_causal_conv_step",
@@ -428,11 +428,9 @@ def swr_selective_scan_backward(x, dt, A, B, C, dy, carriers, D=None, z=None, dt
     p, q = _scan(x, dt, A, B, C, D, z, dt_bias, softplus, h0, lengths)
     dev, lib = x.device, _lib()
     if carriers is None:
-        carriers = _carriers(p, dev)
-        nbytes = _check(lib.swr_selective_scan_workspace_bytes(ctypes.byref(p)), "swr_selective_scan_workspace_bytes")
-        _check(lib.swr_selective_scan(ctypes.byref(p), ctypes.byref(q), None, _ptr(carriers), None,
-                                      _ptr(_workspace(nbytes, None, dev, stream)), _stream(stream, dev)),
-               "swr_selective_scan")
+        with _on(stream, dev):   # (let go when this call returns)
+            _, carriers, _ = swr_selective_scan(x, dt, A, B, C, D, z, dt_bias, softplus, h0, lengths,
+                                                save_carriers=True, stream=stream)
     carriers = _carriers(p, dev, carriers)
     p.sy_b, p.sy_t = _sequence(dy, "dy", x.shape, x.dtype, dev)
     if dh_last is not None:

@@ -270,3 +270,21 @@ def test_autograd(swr):
     (h * dh).sum().backward()
     check_backward(s, definition({**{k: v.detach() for k, v in leaves.items()}, "lengths": None}),
                    [leaves[k].grad for k in order], torch.zeros_like(dy), dh)
+
+
+def test_far_rows(swr):
+    """Tokens so far apart that a tile of them passes 31 bits of bytes."""
+    B, T, D, N = 1, 40, 6, 16
+    s = make(21, B, T, D, N, 1, BF16)
+    far = torch.zeros((T, (1 << 22) + 64), dtype=BF16, device="cuda")
+    far[:, :D] = s["x"][0]
+    want = swr.swr_selective_scan(**s, save_carriers=True, want_state=True)
+    s["x"] = far[None, :, :D]
+    r = definition(s)
+    y, carriers, h = swr.swr_selective_scan(**s, save_carriers=True, want_state=True)
+    check_forward(r, y, h, carriers)
+    check_forward(r, want[0], want[2], want[1])
+    dy = rand(22, (B, T, D), BF16).cuda()
+    got = swr.swr_selective_scan_backward(s["x"], s["dt"], s["A"], s["B"], s["C"], dy, carriers, s["D"], s["z"],
+                                          s["dt_bias"])
+    check_backward(s, r, got, dy)
