@@ -4,12 +4,13 @@
 //     g = dy sigma (1 + pre (1 - sigma));   dx[t] = sum_k w[k] g[t + K - 1 - k];
 //     dw[k] = sum_t g[t] x[t - K + 1 + k];  dbias = sum_t g[t]
 //
-// A thread has 16 bytes of channels of a run of tokens: weights in registers, the
+// A thread has four channels of a run of tokens: weights in registers, the
 // last K - 1 rows of x (and of g) in a window that moves along, so that every row is
 // loaded once but for the K - 1 before (and after) the run.
 //
 // What bounds it is the bytes.
 #include <algorithm>
+#include <type_traits>
 
 #include "swr_lm_launch.h"
 #include "swr_vectors.h"
@@ -19,8 +20,7 @@ namespace {
 
 constexpr int kRun = 16;            // tokens of a thread, forward
 constexpr int kBackRun = 32;        // ... backward
-constexpr int kGroup = 8;           // rows loaded ahead
-constexpr int kBackGroup = 4;
+constexpr int kBackGroup = 4;       // tokens that the backward loads ahead
 constexpr int64_t kMostY = 32768;   // blocks of a launch in y, which take units in turn
 
 __device__ inline float sigmoid(float v) {
@@ -31,14 +31,58 @@ __device__ inline int64_t tokens_of(const ConvParams& p, int64_t b) {
     return p.lengths ? min(max((int64_t)p.lengths[b], (int64_t)0), p.T) : p.T;
 }
 
+// NE channels of a row as they lie in memory; without WHOLE as many of them as there are, and zeros.
+template <class E, int NE>
+struct Row {
+    typedef typename E::store T;
+    static constexpr int kWords = NE * (int)sizeof(T) / 4;
+    struct __attribute__((packed, aligned(sizeof(T)))) Loose {
+        uint32_t w[kWords];
+    };
+    uint32_t w[kWords];
+    template <bool WHOLE>
+    __device__ void load(const T* p, int n) {
+        if constexpr (WHOLE) {
+            const Loose v = *(const Loose*)p;
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = v.w[i];
+        } else {
+            T t[NE] = {};
+#pragma unroll
+            for (int i = 0; i < NE; ++i)
+                if (i < n) t[i] = p[i];
+            __builtin_memcpy(w, t, sizeof w);
+        }
+    }
+    __device__ float operator[](int i) const {
+        if constexpr (sizeof(T) == 4) return as_float(w[i]);
+        else return as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    }
+    template <bool WHOLE>
+    static __device__ void store(T* p, int n, const float* f) {
+        T t[NE];
+#pragma unroll
+        for (int i = 0; i < NE; ++i) t[i] = E::to(f[i]);
+        if constexpr (WHOLE) {
+            Loose v;
+            __builtin_memcpy(&v, t, sizeof v);
+            *(Loose*)p = v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < NE; ++i)
+                if (i < n) p[i] = t[i];
+        }
+    }
+};
+
 // A channel's weights, and its bias.
-template <class E, int K>
+template <class E, int NE, int K>
 struct Taps {
-    float w[E::NE][K], bias[E::NE];
+    float w[NE][K], bias[NE];
     __device__ Taps(const ConvParams& p, int64_t c) {
         const typename E::store* row = (const typename E::store*)p.w + c * K;
 #pragma unroll
-        for (int i = 0; i < E::NE; ++i) {
+        for (int i = 0; i < NE; ++i) {
             const bool there = c + i < p.C;
 #pragma unroll
             for (int k = 0; k < K; ++k) w[i][k] = there ? E::one(row[i * K + k]) : 0.0f;
@@ -48,149 +92,177 @@ struct Taps {
 };
 
 // A block's threads: 1 << shift of them along the channels, the others along the units (runs of
-// tokens, of batch after batch).
-template <class E, int K>
+// tokens, of batch after batch).  A whole run (of tokens and of channels) has no branches, so that its loads
+// go ahead of its stores.
+template <class E, int NE, int K, bool WHOLE, bool SILU>
 __global__ __launch_bounds__(256) void swr_conv_kernel(ConvParams p, int shift, int64_t runs) {
     typedef typename E::store T;
-    typedef Slice<E, E::NE> Row;
-    const int64_t c = ((int64_t)blockIdx.x * (1 << shift) + (threadIdx.x & ((1 << shift) - 1))) * E::NE;
+    typedef Row<E, NE> R;
+    const int64_t c = ((int64_t)blockIdx.x * (1 << shift) + (threadIdx.x & ((1 << shift) - 1))) * NE;
     if (c >= p.C) return;
-    const int n = (int)min(p.C - c, (int64_t)E::NE);
-    const Taps<E, K> taps(p, c);
+    const int n = (int)min(p.C - c, (int64_t)NE);
+    const Taps<E, NE, K> taps(p, c);
     const int64_t per_block = 256 >> shift;
     for (int64_t u = blockIdx.y * per_block + (threadIdx.x >> shift); u < p.B * runs; u += gridDim.y * per_block) {
         const int64_t b = u / runs, first = (u - b * runs) * kRun, end = min(first + kRun, p.T), live = tokens_of(p, b);
-        const T* x = (const T*)p.x + b * p.sx_b;
+        const T* x = (const T*)p.x + b * p.sx_b + c;
         T* y = (T*)p.y + b * p.sy_b + c;
-        const T* state = p.state ? (const T*)p.state + b * (K - 1) * p.C : nullptr;
-        // Rows t - K + 1 .. t of x; before the first token those of the state.
-        Row window[K];
-        const auto fetch = [&](int64_t t) {
-            Row r = {};
-            if (t >= 0) {
-                if (t < live && t < end) r.load(x + t * p.sx_t, (int)c, (int)p.C);
-            } else if (state && t >= 1 - K) {
-                r.load(state + (K - 1 + t) * p.C, (int)c, (int)p.C);
-            }
-            return r;
-        };
+        const T* state = p.state ? (const T*)p.state + b * (K - 1) * p.C + c : nullptr;
+        // Rows before the run, of the state before the first token.
+        R window[K];
 #pragma unroll
-        for (int k = 0; k + 1 < K; ++k) window[k + 1] = fetch(first + k - K + 1);
-        Row kept[K];   // the state's rows that the new state may still need
+        for (int k = 0; k + 1 < K; ++k) {
+            const int64_t t = first + k - K + 1;
+            window[k + 1] = {};
+            if (t >= 0 && t < live) window[k + 1].template load<WHOLE>(x + t * p.sx_t, n);
+            if (t < 0 && state) window[k + 1].template load<WHOLE>(state + (K - 1 + t) * p.C, n);
+        }
+        R kept[K];   // the state's rows that the new state may still need
         if (K > 1 && p.state_out && first == 0) {
 #pragma unroll
             for (int k = 0; k + 1 < K; ++k) {
                 const int64_t t = live + k - K + 1;
                 kept[k] = {};
-                if (t >= 0) kept[k].load(x + t * p.sx_t, (int)c, (int)p.C);
-                else if (state) kept[k].load(state + (K - 1 + t) * p.C, (int)c, (int)p.C);
+                if (t >= 0) kept[k].template load<WHOLE>(x + t * p.sx_t, n);
+                else if (state) kept[k].template load<WHOLE>(state + (K - 1 + t) * p.C, n);
             }
         }
-        for (int64_t t = first; t < end; t += kGroup) {
-            Row next[kGroup];
+        const auto run = [&](auto whole) {
+            constexpr bool kAll = whole;
+            R rows[kRun];
 #pragma unroll
-            for (int i = 0; i < kGroup; ++i) next[i] = fetch(t + i);
+            for (int i = 0; i < kRun; ++i)
+                if (kAll || first + i < live) rows[i].template load<WHOLE>(x + (first + i) * p.sx_t, n);
+                else rows[i] = {};
 #pragma unroll
-            for (int i = 0; i < kGroup; ++i) {
+            for (int i = 0; i < kRun; ++i) {
 #pragma unroll
                 for (int k = 0; k + 1 < K; ++k) window[k] = window[k + 1];
-                window[K - 1] = next[i];
-                float f[E::NE];
+                window[K - 1] = rows[i];
+                float f[NE];
 #pragma unroll
-                for (int e = 0; e < E::NE; ++e) {
+                for (int e = 0; e < NE; ++e) {
                     float pre = taps.bias[e];
 #pragma unroll
                     for (int k = 0; k < K; ++k) pre = fmaf(taps.w[e][k], window[k][e], pre);
-                    f[e] = p.silu ? pre * sigmoid(pre) : pre;
-                    if (t + i >= live) f[e] = 0.0f;
+                    f[e] = SILU ? pre * sigmoid(pre) : pre;
+                    if (!kAll && first + i >= live) f[e] = 0.0f;
                 }
-                if (t + i < end) store<E, E::NE>(y + (t + i) * p.sy_t, n, f);
+                if (kAll || first + i < end) R::template store<WHOLE>(y + (first + i) * p.sy_t, n, f);
             }
-        }
+        };
+        if (first + kRun <= live) run(std::true_type());
+        else run(std::false_type());
         if (K > 1 && p.state_out && first == 0) {
 #pragma unroll
             for (int k = 0; k + 1 < K; ++k) {
-                float f[E::NE];
+                float f[NE];
 #pragma unroll
-                for (int e = 0; e < E::NE; ++e) f[e] = kept[k][e];
-                store<E, E::NE>((T*)p.state_out + (b * (K - 1) + k) * p.C + c, n, f);
+                for (int e = 0; e < NE; ++e) f[e] = kept[k][e];
+                R::template store<WHOLE>((T*)p.state_out + (b * (K - 1) + k) * p.C + c, n, f);
             }
         }
     }
 }
 
-// Backward.  A block's 64 threads along the channels take every gridDim.y-th four runs, one for each of
-// its waves; the waves' shares of dw and dbias are added in LDS, in order, and written as one row of `partial`.
-template <class E, int K>
+// Backward.  A block's 64 threads along the channels, four channels each, take every gridDim.y-th four runs, one for
+// each of its waves; the waves' shares of dw and dbias are added in LDS, in order, and written as one row of `partial`.
+// (With eight bf16 channels a thread, of 272 registers, 5 x 4099 x 4096 took 274 us.)
+template <class E, int NE, int K, bool WHOLE, bool SILU>
 __global__ __launch_bounds__(256) void swr_conv_back_kernel(ConvParams p, int64_t runs) {
     typedef typename E::store T;
-    typedef Slice<E, E::NE> Row;
-    __shared__ float share[64 * E::NE * (K + 1)];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * E::NE;
-    const int n = (int)max(min(p.C - c, (int64_t)E::NE), (int64_t)0);
-    float sums[E::NE][K + 1] = {};
+    typedef Row<E, NE> R;
+    __shared__ float share[64 * NE * (K + 1)];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * NE;
+    // (Rows are a wave's: their addresses are scalars, a lane adds 32 bits.)
+    const uint32_t bytes = (uint32_t)c * (uint32_t)sizeof(T);
+    const auto at_lane = [&](auto* row) { return (decltype(row))((const char*)row + bytes); };
+    const int n = (int)max(min(p.C - c, (int64_t)NE), (int64_t)0);
+    float sums[NE][K + 1] = {};
     if (n > 0) {
-        const Taps<E, K> taps(p, c);
+        const Taps<E, NE, K> taps(p, c);
         for (int64_t u = blockIdx.y * 4 + wave; u < p.B * runs; u += gridDim.y * 4) {
-            const int64_t b = u / runs, first = (u - b * runs) * kBackRun, end = min(first + kBackRun, p.T);
-            const int64_t live = tokens_of(p, b);
+            const int64_t b = u / runs;
+            const int first = (int)(u - b * runs) * kBackRun, end = (int)min((int64_t)first + kBackRun, p.T);
+            const int live = __builtin_amdgcn_readfirstlane((int)tokens_of(p, b));
             const T* x = (const T*)p.x + b * p.sx_b;
             const T* dy = (const T*)p.dy + b * p.sy_b;
-            T* dx = (T*)p.dx + b * p.sd_b + c;
-            Row window[K];
-            float g[K][E::NE] = {};   // of the tokens t - K + 1 .. t
-            const auto fetch = [&](const T* rows, int64_t stride, int64_t t) {
-                Row r = {};
-                if (t >= 0 && t < live && t < end + K - 1) r.load(rows + t * stride, (int)c, (int)p.C);
-                return r;
-            };
+            T* dx = (T*)p.dx + b * p.sd_b;
+            if (first >= live) {   // nothing there
+                const float zeros[NE] = {};
+                for (int t = first; t < end; ++t) R::template store<WHOLE>(at_lane(dx + t * p.sd_t), n, zeros);
+                continue;
+            }
+            R window[K];
+            float g[K][NE] = {};   // of the tokens t - K + 1 .. t
 #pragma unroll
-            for (int k = 0; k + 1 < K; ++k) window[k + 1] = fetch(x, p.sx_t, first + k - K + 1);
-            // The token t takes part in the gradients of x at t - K + 1 .. t.
-            for (int64_t t = first; t < end + K - 1; t += kBackGroup) {
-                Row xs[kBackGroup], ds[kBackGroup];
+            for (int k = 0; k + 1 < K; ++k) {
+                const int t = first + k - K + 1;
+                window[k + 1] = {};
+                if (t >= 0) window[k + 1].template load<WHOLE>(at_lane(x + t * p.sx_t), n);
+            }
+            struct Group {
+                R x[kBackGroup], dy[kBackGroup];
+            } even, odd;
+            const int last = live - 1;
+            const auto fetch = [&](Group& v, int t) {   // (past the last token that one once more)
 #pragma unroll
                 for (int i = 0; i < kBackGroup; ++i) {
-                    xs[i] = fetch(x, p.sx_t, t + i);
-                    ds[i] = fetch(dy, p.sy_t, t + i);
+                    const int at = min(t + i, last);
+                    v.x[i].template load<WHOLE>(at_lane(x + at * p.sx_t), n);
+                    v.dy[i].template load<WHOLE>(at_lane(dy + at * p.sy_t), n);
                 }
+            };
+            // The token t takes part in the gradients of x at t - K + 1 .. t.
+            const auto step = [&](const Group& v, int t) {
 #pragma unroll
                 for (int i = 0; i < kBackGroup; ++i) {
                     const bool there = t + i < live, own = t + i < end;
 #pragma unroll
                     for (int k = 0; k + 1 < K; ++k) window[k] = window[k + 1];
-                    window[K - 1] = xs[i];
-                    float f[E::NE];
+                    window[K - 1] = v.x[i];
+                    float f[NE];
 #pragma unroll
-                    for (int e = 0; e < E::NE; ++e) {
-                        float pre = taps.bias[e], v = ds[i][e];
+                    for (int e = 0; e < NE; ++e) {
+                        float pre = taps.bias[e], d = v.dy[i][e];
 #pragma unroll
                         for (int k = 0; k < K; ++k) pre = fmaf(taps.w[e][k], window[k][e], pre);
-                        if (p.silu) {
+                        if constexpr (SILU) {
                             const float gate = sigmoid(pre);
-                            v *= gate * fmaf(pre, 1.0f - gate, 1.0f);
+                            d *= gate * fmaf(pre, 1.0f - gate, 1.0f);
                         }
-                        if (!there) v = 0.0f;
+                        if (!there) d = 0.0f;
 #pragma unroll
                         for (int k = 0; k + 1 < K; ++k) g[k][e] = g[k + 1][e];
-                        g[K - 1][e] = v;
-                        const float mine = own ? v : 0.0f;
+                        g[K - 1][e] = d;
+                        const float mine = own ? d : 0.0f;
 #pragma unroll
-                        for (int k = 0; k < K; ++k) sums[e][k] = fmaf(mine, window[k][e], sums[e][k]);
+                        for (int k = 0; k < K; ++k) {
+                            // (past the last token the window holds it again, which may be infinite)
+                            const float xe = there ? window[k][e] : 0.0f;
+                            sums[e][k] = fmaf(mine, xe, sums[e][k]);
+                        }
                         sums[e][K] += mine;
                         // dx[t - K + 1] = sum_k w[k] g[t - k]
                         f[e] = 0.0f;
 #pragma unroll
                         for (int k = 0; k < K; ++k) f[e] = fmaf(taps.w[e][k], g[K - 1 - k][e], f[e]);
                     }
-                    const int64_t at = t + i - K + 1;
+                    const int at = t + i - K + 1;
                     if (at >= live) {
 #pragma unroll
-                        for (int e = 0; e < E::NE; ++e) f[e] = 0.0f;
+                        for (int e = 0; e < NE; ++e) f[e] = 0.0f;
                     }
-                    if (at >= first && at < end) store<E, E::NE>(dx + at * p.sd_t, n, f);
+                    if (at >= first && at < end) R::template store<WHOLE>(at_lane(dx + at * p.sd_t), n, f);
                 }
+            };
+            fetch(even, first);
+            for (int t = first; t < end + K - 1; t += 2 * kBackGroup) {
+                fetch(odd, t + kBackGroup);
+                step(even, t);
+                fetch(even, t + 2 * kBackGroup);
+                step(odd, t + kBackGroup);
             }
         }
     }
@@ -199,7 +271,7 @@ __global__ __launch_bounds__(256) void swr_conv_back_kernel(ConvParams p, int64_
         __syncthreads();
         if (wave == w) {
 #pragma unroll
-            for (int e = 0; e < E::NE; ++e)
+            for (int e = 0; e < NE; ++e)
 #pragma unroll
                 for (int k = 0; k <= K; ++k) {
                     float* s = share + (e * (K + 1) + k) * 64 + lane;
@@ -211,7 +283,7 @@ __global__ __launch_bounds__(256) void swr_conv_back_kernel(ConvParams p, int64_
     if (wave == 3) {
         float* out = p.partial + (blockIdx.y * p.C + c) * (K + 1);
 #pragma unroll
-        for (int e = 0; e < E::NE; ++e)
+        for (int e = 0; e < NE; ++e)
 #pragma unroll
             for (int k = 0; k <= K; ++k)
                 if (e < n) out[e * (K + 1) + k] = sums[e][k];
@@ -261,29 +333,42 @@ hipError_t by_taps(int taps, const F<E, 1>&, const ConvParams& p, hipStream_t st
 template <class E, int K>
 struct Forward {
     static hipError_t run(const ConvParams& p, hipStream_t st) {
-        const int64_t vectors = (p.C + E::NE - 1) / E::NE, runs = std::max<int64_t>(1, (p.T + kRun - 1) / kRun);
+        constexpr int NE = 4;
+        const int64_t vectors = (p.C + NE - 1) / NE, runs = std::max<int64_t>(1, (p.T + kRun - 1) / kRun);
         int shift = 0;
         while (shift < 8 && ((int64_t)1 << shift) < vectors) ++shift;
         const int64_t units = (p.B * runs + (256 >> shift) - 1) / (256 >> shift);
-        hipLaunchKernelGGL((swr_conv_kernel<E, K>),
-                           dim3((unsigned)((vectors + (1 << shift) - 1) >> shift), (unsigned)std::min(units, kMostY)),
-                           dim3(256), 0, st, p, shift, runs);
+        const dim3 grid((unsigned)((vectors + (1 << shift) - 1) >> shift), (unsigned)std::min(units, kMostY));
+        const auto kernel = p.C % NE == 0 ? p.silu ? swr_conv_kernel<E, NE, K, true, true>
+                                                   : swr_conv_kernel<E, NE, K, true, false>
+                                          : p.silu ? swr_conv_kernel<E, NE, K, false, true>
+                                                   : swr_conv_kernel<E, NE, K, false, false>;
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, p, shift, runs);
         return hipGetLastError();
     }
 };
 
+constexpr int kBackChannels = 4;   // of a thread
+
 // Rows of partial sums: as many blocks as fill the GPU and no more than there are fours of runs.
-int64_t back_rows(int64_t B, int64_t T, int64_t C, int ne) {
-    const int64_t fours = (B * ((T + kBackRun - 1) / kBackRun) + 3) / 4, along = (C + 64 * ne - 1) / (64 * ne);
+int64_t back_rows(int64_t B, int64_t T, int64_t C) {
+    const int64_t fours = (B * ((T + kBackRun - 1) / kBackRun) + 3) / 4, along = (C + 64 * kBackChannels - 1) /
+                                                                                  (64 * kBackChannels);
     return std::max<int64_t>(1, std::min(fours, std::max<int64_t>(1, (1536 + along - 1) / along)));
 }
 
 template <class E, int K>
 struct Backward {
     static hipError_t run(const ConvParams& p, hipStream_t st) {
-        const int64_t along = (p.C + 64 * E::NE - 1) / (64 * E::NE), rows = back_rows(p.B, p.T, p.C, E::NE);
-        hipLaunchKernelGGL((swr_conv_back_kernel<E, K>), dim3((unsigned)along, (unsigned)rows), dim3(256), 0, st, p,
-                           (p.T + kBackRun - 1) / kBackRun);
+        constexpr int NE = kBackChannels;
+        const int64_t along = (p.C + 64 * NE - 1) / (64 * NE), rows = back_rows(p.B, p.T, p.C);
+        const int64_t runs = (p.T + kBackRun - 1) / kBackRun;
+        const dim3 grid((unsigned)along, (unsigned)rows);
+        const auto kernel = p.C % NE == 0 ? p.silu ? swr_conv_back_kernel<E, NE, K, true, true>
+                                                   : swr_conv_back_kernel<E, NE, K, true, false>
+                                          : p.silu ? swr_conv_back_kernel<E, NE, K, false, true>
+                                                   : swr_conv_back_kernel<E, NE, K, false, false>;
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, p, runs);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         const int64_t blocks = std::min<int64_t>((p.C * (K + 1) + 63) / 64, 1 << 20);
@@ -299,8 +384,8 @@ hipError_t launch_conv(int dtype, int taps, const ConvParams& p, void* stream) {
     return dtype == SWR_DTYPE_F32 ? by_taps<Forward, F32>(taps, {}, p, st) : by_taps<Forward, Bf16>(taps, {}, p, st);
 }
 
-int64_t conv_work_bytes(int dtype, int64_t B, int64_t T, int64_t C, int taps) {
-    return back_rows(B, T, C, dtype == SWR_DTYPE_F32 ? F32::NE : Bf16::NE) * C * (taps + 1) * 4;
+int64_t conv_work_bytes(int64_t B, int64_t T, int64_t C, int taps) {
+    return back_rows(B, T, C) * C * (taps + 1) * 4;
 }
 
 hipError_t launch_conv_backward(int dtype, int taps, const ConvParams& p, void* stream) {

@@ -261,7 +261,7 @@ int swr_causal_conv(const swr_conv_t* p, const void* x, const void* w, const voi
 int64_t swr_causal_conv_workspace_bytes(const swr_conv_t* p) {
     ConvSizes s;
     const int rc = resolve(p, true, &s);
-    return rc != SWR_OK ? rc : swr::conv_work_bytes(p->dtype, p->B, p->T, p->C, p->taps);
+    return rc != SWR_OK ? rc : swr::conv_work_bytes(p->B, p->T, p->C, p->taps);
 }
 
 int swr_causal_conv_backward(const swr_conv_t* p, const void* x, const void* w, const void* bias, const void* dy,
@@ -274,7 +274,7 @@ int swr_causal_conv_backward(const swr_conv_t* p, const void* x, const void* w, 
     if (!all_aligned({x, w, bias, dy, dx}, size_of(p->dtype)) || !all_aligned({lengths, dw, dbias}, 4) ||
         !aligned(workspace, 16))
         return SWR_ERR_ALIGN;
-    const int64_t work = swr::conv_work_bytes(p->dtype, p->B, p->T, p->C, p->taps);
+    const int64_t work = swr::conv_work_bytes(p->B, p->T, p->C, p->taps);
     if (clashes({span(dx, s.dx), span(dw, p->C * p->taps * 4), span(dbias, p->C * 4), span(workspace, work)},
                 {span(x, s.x), span(w, s.w), span(bias, s.bias), span(dy, s.y), span(lengths, s.lengths)}))
         return SWR_ERR_ALIAS;

@@ -34,7 +34,7 @@ struct ConvParams {
     bool silu;
 };
 hipError_t launch_conv(int dtype, int taps, const ConvParams& p, void* stream);
-int64_t conv_work_bytes(int dtype, int64_t B, int64_t T, int64_t C, int taps);
+int64_t conv_work_bytes(int64_t B, int64_t T, int64_t C, int taps);
 hipError_t launch_conv_backward(int dtype, int taps, const ConvParams& p, void* stream);
 
 // Channels of a block of threads, and runs of tokens that the work is cut into.
