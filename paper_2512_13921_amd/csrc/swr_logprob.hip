@@ -10,9 +10,9 @@
 // (m is subtracted first: of logits that are all a type's lowest value, as a mask leaves them, the
 // products would overflow, and of large ones lose what differs.)
 //
-// Alternatives: a wave keeps the largest (logit, token) that it has met in its lanes, the largest
-// first, and looks at a tile of logits one by one only where some lane's largest
-// reaches the last of them.  The first tile's lanes' largest, sorted, give a bound to begin with.
+// Alternatives: of the threads' largest logits the one of order `top` is a bound that as many logits reach, and few
+// more: the few threads that have some look through theirs once more and put them into a list, which is
+// then ranked.  (With sorted lists that took in logits as they were met, 8 rows of 65536 took 40 us.)
 //
 // The gradient reads the logits again:
 //     dlogits = scale p (dlse - dlogp - dentropy (log p + entropy)) + scale dlogp at the token
@@ -21,6 +21,7 @@
 // which the exponential counts four.
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 #include "swr_lm_launch.h"
 #include "swr_vectors.h"
@@ -54,6 +55,17 @@ __device__ inline Sums join(Sums a, Sums b, float k) {
     return {m, a.s + b.s, a.u + b.u};
 }
 
+// ... of a wave's lanes; every lane adds in the same order.
+__device__ inline Sums wave_join(Sums a, float k) {
+    const int lane = threadIdx.x % 64;
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) {
+        const Sums b{__shfl_xor(a.m, m), __shfl_xor(a.s, m), __shfl_xor(a.u, m)};
+        a = lane & m ? join(b, a, k) : join(a, b, k);
+    }
+    return a;
+}
+
 // A logit's and its token's place in the order of alternatives: a larger key is better.  NaN is above
 // all numbers, zeros are equal, and of equal logits the lower token is better.
 __device__ inline uint32_t ordered(float x) {
@@ -65,36 +77,33 @@ __device__ inline uint32_t ordered(float x) {
 __device__ inline float unordered(uint32_t k) {
     return as_float(k == 0xffffffffu ? 0x7fc00000u : k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
-__device__ inline uint64_t key_of(float x, uint32_t token) { return (uint64_t)ordered(x) << 32 | (uint32_t)~token; }
+__device__ inline uint32_t partner(uint32_t v, int reach) { return (uint32_t)__shfl_xor((int)v, reach); }
+__device__ inline uint64_t partner(uint64_t v, int reach) { return (uint64_t)__shfl_xor((long long)v, reach); }
 
-__device__ inline uint64_t lane_of(uint64_t v, int lane) {
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
-           (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
-}
-
-// A wave's best, the largest key in lane 0.
-struct Best {
-    uint64_t key = 0, last = 0;   // last: of lane top - 1; less than every key while there are fewer
-    __device__ void insert(uint64_t k, int top) {
-        const int at = __popcll(__ballot(key > k)), lane = threadIdx.x % 64;
-        const uint64_t up = __shfl_up(key, 1);
-        key = lane < at ? key : lane == at ? k : up;
-        last = lane_of(key, top - 1);
-    }
-};
-
-// The value of order `top` among a wave's 64, the largest first.
-__device__ inline uint32_t order_statistic(uint32_t v, int top) {
+// A wave's 64 values in its lanes, the largest first.
+__device__ inline uint32_t sorted(uint32_t v) {
     const int lane = threadIdx.x % 64;
 #pragma unroll
     for (int size = 2; size <= 64; size *= 2)
 #pragma unroll
         for (int reach = size / 2; reach > 0; reach /= 2) {
-            const uint32_t other = (uint32_t)__shfl_xor((int)v, reach);
+            const uint32_t other = partner(v, reach);
             const bool down = (lane & size) == 0, low = (lane & reach) == 0;
             v = down == low ? max(v, other) : min(v, other);
         }
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, top - 1);
+    return v;
+}
+// The 64 largest of two such lists, of the second in reverse (its last value in lane 0).
+template <class T>
+__device__ inline T merged(T v, T reverse) {
+    const int lane = threadIdx.x % 64;
+    v = max(v, reverse);
+#pragma unroll
+    for (int reach = 32; reach > 0; reach /= 2) {
+        const T other = partner(v, reach);
+        v = lane & reach ? min(v, other) : max(v, other);
+    }
+    return v;
 }
 
 // What a block leaves of its part of a row: sums, and its best keys.
@@ -127,17 +136,119 @@ __device__ inline int64_t token_of(const LogProbParams& p, int64_t row) {
     return p.wide_tokens ? ((const int64_t*)p.tokens)[row] : ((const int32_t*)p.tokens)[row];
 }
 
-// Writes the `top` largest of n keys in LDS, each to its place: as many as are larger.
-__device__ inline void write_best(const LogProbParams& p, int64_t row, const uint64_t* keys, int n, int thread, int threads,
-                                  const Row& r) {
-    for (int i = thread; i < n; i += threads) {
-        const uint64_t own = keys[i];
-        if (own == 0) continue;   // (a place that no logit took)
-        int at = 0;
-        for (int k = 0; k < n; ++k) at += keys[k] > own;
-        if (at >= p.top) continue;
-        p.top_logp[row * p.top + at] = r.log(unordered((uint32_t)(own >> 32)));
-        p.top_tokens[row * p.top + at] = (int64_t)(uint32_t)~(uint32_t)own;
+// How many of n keys are larger.
+__device__ inline int rank_of(const uint64_t* keys, int n, uint64_t own) {
+    int at = 0;
+#pragma unroll 8
+    for (int k = 0; k < n; ++k) at += keys[k] > own;
+    return at;
+}
+__device__ inline void write_one(const LogProbParams& p, int64_t row, int at, uint64_t key, const Row& r) {
+    p.top_logp[row * p.top + at] = r.log(unordered((uint32_t)(key >> 32)));
+    p.top_tokens[row * p.top + at] = (int64_t)(uint32_t)~(uint32_t)key;
+}
+
+// The lists that a row's alternatives are found with: logits above the bound, and equal to it.
+constexpr int kAbove = 1024, kEqual = 256;
+template <int WAVES>
+struct Lists {
+    uint64_t above[WAVES == 1 ? 512 : kAbove], equal[kEqual];
+    uint32_t largest[WAVES == 1 ? 1 : WAVES][64];   // the waves' lists
+    int counts[WAVES];
+    int above_n, equal_n;
+    uint32_t bound;
+    static constexpr int kMost = WAVES == 1 ? 512 : kAbove;
+};
+
+// The threads of a row wait for each other.
+template <int WAVES>
+__device__ inline void meet() {
+    if constexpr (WAVES == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup"), __builtin_amdgcn_wave_barrier();
+    else __syncthreads();
+}
+
+// The `top` largest keys of the elements first .. last - 1 of a row, in any order of the row's threads: f(rank, key)
+// for each, where there are as many.  `own`: the largest of the thread's own, 0 without any.
+template <class E, int WAVES, class F>
+__device__ inline void find_best(const typename E::store* x, int64_t first, int64_t last, int top, uint32_t own, int t,
+                                 Lists<WAVES>& l, F f) {
+    constexpr int NE = E::NE, kThreads = 64 * WAVES;
+    const int lane = threadIdx.x % 64, wave = t / 64;
+    uint32_t in_order = sorted(own);
+    for (int step = WAVES / 2; step > 0; step /= 2) {
+        if (wave < 2 * step) l.largest[wave][lane] = in_order;
+        __syncthreads();
+        if (wave < step) in_order = merged(in_order, l.largest[wave + step][63 - lane]);
+        __syncthreads();
+    }
+    if (t == top - 1) l.bound = in_order;
+    for (;;) {
+        if (t == 0) l.above_n = l.equal_n = 0;
+        meet<WAVES>();
+        const uint32_t bound = l.bound;
+        // A wave looks through the elements of those of its lanes that have some, one lane's after the other's:
+        // short code, as it runs once (unrolled, it took 5 us more, to be fetched).
+        for (uint64_t todo = __ballot(own >= bound && own > 0); todo; todo &= todo - 1) {
+            const int64_t who = first + ((int64_t)wave * 64 + __builtin_ctzll(todo)) * NE;
+#pragma unroll 1
+            for (int64_t from = 0; who + from * kThreads < last; from += 64) {
+                const int64_t e = who + (from + lane / NE * NE) * kThreads + lane % NE;
+                const uint32_t v = e < last ? ordered(E::one(x[e])) : 0;
+                const uint64_t key = (uint64_t)v << 32 | (uint32_t)~(uint32_t)e, before = ((uint64_t)1 << lane) - 1;
+                const uint64_t more = __ballot(v > bound), same = __ballot(v == bound && e < last);
+                int to = 0;
+                if (lane == 0 && more) to = atomicAdd(&l.above_n, __popcll(more));
+                to = __builtin_amdgcn_readfirstlane(to) + __popcll(more & before);
+                if (v > bound && to < Lists<WAVES>::kMost) l.above[to] = key;
+                if (lane == 0 && same) to = atomicAdd(&l.equal_n, __popcll(same));
+                to = __builtin_amdgcn_readfirstlane(to) + __popcll(same & before);
+                if (v == bound && e < last && to < kEqual) l.equal[to] = key;
+            }
+        }
+        meet<WAVES>();
+        const int above = l.above_n, equal = l.equal_n;
+        if (above > Lists<WAVES>::kMost) {   // too many: the bound of order `top` among those that are listed
+            for (int i = t; i < Lists<WAVES>::kMost; i += kThreads)
+                if (rank_of(l.above, Lists<WAVES>::kMost, l.above[i]) == top - 1) l.bound = (uint32_t)(l.above[i] >> 32);
+            meet<WAVES>();
+            continue;
+        }
+        int ties = equal;
+        if (equal > kEqual) {   // many equal ones: the first of them, in order
+            const int need = max(top - above, 0);
+            int so_far = 0;
+            for (int64_t base = first; base < last && so_far < need; base += kThreads) {
+                const int64_t e = base + t;
+                const bool is = e < last && ordered(E::one(x[min(e, last - 1)])) == bound;
+                const uint64_t mask = __ballot(is);
+                int before = so_far, all = __popcll(mask);
+                if constexpr (WAVES > 1) {
+                    if (lane == 0) l.counts[wave] = all;
+                    __syncthreads();
+                    all = 0;
+                    for (int w = 0; w < WAVES; ++w) {
+                        before += w < wave ? l.counts[w] : 0;
+                        all += l.counts[w];
+                    }
+                    __syncthreads();
+                }
+                before += __popcll(mask & (((uint64_t)1 << lane) - 1));
+                if (is && before < need) l.equal[before] = (uint64_t)bound << 32 | (uint32_t)~(uint32_t)e;
+                so_far += all;
+            }
+            ties = min(so_far, need);
+            meet<WAVES>();
+        }
+        for (int i = t; i < above; i += kThreads) {
+            const int at = rank_of(l.above, above, l.above[i]);
+            if (at < top) f(at, l.above[i]);
+        }
+        for (int i = t; i < ties; i += kThreads) {
+            const int at = above + rank_of(l.equal, ties, l.equal[i]);
+            if (at < top) f(at, l.equal[i]);
+        }
+        meet<WAVES>();   // (the lists have been read)
+        return;
     }
 }
 
@@ -148,12 +259,12 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void swr_logprob_ker
     constexpr int NE = E::NE, kVectors = kTileVectors, kTile = NE * kVectors;
     constexpr int kLists = WAVES == 1 ? 4 : WAVES;
     __shared__ Sums sums[kLists];
-    __shared__ uint64_t best_keys[TOP ? kLists * SWR_TOP_MOST : 1];
+    struct None {};
+    __shared__ std::conditional_t<TOP, Lists<WAVES>, None> lists[TOP && WAVES == 1 ? 4 : 1];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int t = WAVES == 1 ? lane : threadIdx.x, size = 64 * WAVES;
     const float k = p.scale * kLog2e;
     const int64_t items = p.rows * p.parts, step = WAVES == 1 ? gridDim.x * 4 : gridDim.x;
-    // (Waves of a block with rows of their own go as often round as each other: barriers.)
     for (int64_t base = WAVES == 1 ? blockIdx.x * 4 : blockIdx.x; base < items; base += step) {
         const int64_t item = WAVES == 1 ? base + wave : base;
         const bool there = item < items;
@@ -163,7 +274,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void swr_logprob_ker
         const int64_t tiles = (p.vocab + (int64_t)kTile * size - 1) / ((int64_t)kTile * size);
         const int64_t first = there ? tiles * part / p.parts : 0, last = there ? tiles * (part + 1) / p.parts : 0;
         Sums a{-__builtin_inff(), 0.0f, 0.0f};
-        Best best;
+        bool odd = false;   // a NaN, which a maximum passes over
         for (int64_t tile = first; tile < last; ++tile) {
             Slice<E, NE> v[kVectors];
             const int64_t at = tile * kTile * size + (int64_t)t * NE;
@@ -194,104 +305,70 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void swr_logprob_ker
                     a.u = fmaf(e, fmaxf(d, -160.0f), a.u);   // (2^-160 is 0 in float32)
                 }
             if constexpr (TOP) {
-                bool odd = false;   // NaN, which a maximum passes over
 #pragma unroll
                 for (int i = 0; i < kVectors; ++i)
 #pragma unroll
                     for (int c = 0; c < NE; ++c) odd |= v[i][c] != v[i][c];
-                const uint32_t largest = odd ? 0xffffffffu : ordered(top);
-                uint32_t bound = (uint32_t)(best.last >> 32);
-                if (best.last == 0) bound = max(bound, order_statistic(at < p.vocab ? largest : 0, p.top));
-                if (__ballot(largest >= bound && at < p.vocab)) {
-#pragma unroll
-                    for (int i = 0; i < kVectors; ++i)
-#pragma unroll
-                        for (int c = 0; c < NE; ++c) {
-                            const int64_t token = at + (int64_t)i * size * NE + c;
-                            const uint64_t own = key_of(v[i][c], (uint32_t)token);
-                            const bool may = token < p.vocab && (uint32_t)(own >> 32) >= bound;
-                            uint64_t left = __ballot(may && own > best.last);
-                            while (left) {
-                                const uint64_t cand = lane_of(own, __builtin_ctzll(left));
-                                left &= left - 1;
-                                if (cand > best.last) best.insert(cand, p.top);
-                            }
-                        }
-                }
             }
         }
-#pragma unroll
-        for (int m = 32; m > 0; m >>= 1) {
-            const Sums b{__shfl_xor(a.m, m), __shfl_xor(a.s, m), __shfl_xor(a.u, m)};
-            // (both lanes add in the same order)
-            a = lane & m ? join(b, a, k) : join(a, b, k);
-        }
-        uint64_t* own_keys = best_keys + (WAVES == 1 ? wave * SWR_TOP_MOST : 0);
-        if constexpr (TOP) {
-            if (lane < p.top) best_keys[WAVES == 1 ? wave * SWR_TOP_MOST + lane : wave * p.top + lane] = best.key;
-        }
+        const int64_t begin = first * kTile * size, end = min(last * kTile * size, p.vocab);
+        uint32_t largest = 0;
+        if (TOP && begin + (int64_t)t * NE < end) largest = odd ? 0xffffffffu : ordered(a.m);
+        a = wave_join(a, k);
         if constexpr (WAVES > 1) {
             if (lane == 0) sums[wave] = a;
             __syncthreads();
             a = sums[0];
             for (int w = 1; w < WAVES; ++w) a = join(a, sums[w], k);
-        } else if constexpr (TOP) {
-            __syncthreads();
         }
-        const int keys = TOP ? (WAVES == 1 ? 1 : WAVES) * p.top : 0;
         if (there && p.parts == 1) {
             const int64_t token = token_of(p, row);
             const bool scored = token >= 0 && token < p.vocab;
             if (t == 0) finish(p, row, a, scored ? E::one(x[token]) : 0.0f, scored);
             if constexpr (TOP) {
-                write_best(p, row, own_keys, keys, t, size, Row(a, p.scale));
+                const Row r(a, p.scale);
+                find_best<E, WAVES>(x, begin, end, p.top, largest, t, lists[WAVES == 1 ? wave : 0],
+                                    [&](int at, uint64_t key) { write_one(p, row, at, key, r); });
             }
         } else if (there) {
             if (t == 0) *part_of(p.work, row, p.parts, part) = Part{a, 0};
             if constexpr (TOP) {
-                // The part's best, in any order; places that no key takes are 0.
                 uint64_t* out = keys_of(p.work, p.rows, row, p.parts, part, p.top);
-                for (int i = t; i < keys; i += size) {
-                    const uint64_t own = own_keys[i];
-                    int at = 0;
-                    for (int q = 0; q < keys; ++q) at += own_keys[q] > own || (own_keys[q] == own && q < i);
-                    if (at < p.top) out[at] = own;
-                }
+                if (t < p.top) out[t] = 0;   // (a part may have fewer logits)
+                find_best<E, WAVES>(x, begin, end, p.top, largest, t, lists[WAVES == 1 ? wave : 0],
+                                    [&](int at, uint64_t key) { out[at] = key; });
             }
         }
-        if constexpr (WAVES > 1 || TOP) __syncthreads();   // (the LDS has been read)
+        if constexpr (WAVES > 1) __syncthreads();   // (the LDS has been read)
     }
 }
 
-// Rows of several parts: their sums in order, and the best of their best.
+// Rows of several parts: their sums in order, and the best of their best, which four waves merge.
 template <class E, bool TOP>
 __global__ __launch_bounds__(256) void swr_logprob_join_kernel(LogProbParams p) {
-    __shared__ uint64_t list[SWR_TOP_MOST], next[2 * SWR_TOP_MOST];
+    __shared__ uint64_t lists[4][64];
     const float k = p.scale * kLog2e;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
-        Sums a = part_of(p.work, row, p.parts, 0)->sums;
-        for (int i = 1; i < p.parts; ++i) a = join(a, part_of(p.work, row, p.parts, i)->sums, k);
         const int64_t token = token_of(p, row);
         const bool scored = token >= 0 && token < p.vocab;
-        if (threadIdx.x == 0)
-            finish(p, row, a, scored ? E::one(((const typename E::store*)p.logits)[row * p.sl + token]) : 0.0f, scored);
+        const float x = scored ? E::one(((const typename E::store*)p.logits)[row * p.sl + token]) : 0.0f;
+        Sums a{-__builtin_inff(), 0.0f, 0.0f};   // (of at most 64 parts, one a lane)
+        if (lane < p.parts) a = part_of(p.work, row, p.parts, lane)->sums;
+        a = wave_join(a, k);
+        if (threadIdx.x == 0) finish(p, row, a, x, scored);
         if constexpr (TOP) {
-            const int t = threadIdx.x;
-            if (t < p.top) list[t] = keys_of(p.work, p.rows, row, p.parts, 0, p.top)[t];
-            for (int part = 1; part < p.parts; ++part) {
-                __syncthreads();
-                if (t < p.top) next[t] = list[t];
-                else if (t < 2 * p.top) next[t] = keys_of(p.work, p.rows, row, p.parts, part, p.top)[t - p.top];
-                __syncthreads();
-                if (t < 2 * p.top) {
-                    const uint64_t own = next[t];
-                    int at = 0;
-                    for (int q = 0; q < 2 * p.top; ++q) at += next[q] > own || (next[q] == own && q < t);
-                    if (at < p.top) list[at] = own;
-                }
+            uint64_t best = 0;
+            for (int part = wave; part < p.parts; part += 4) {
+                const uint64_t* list = keys_of(p.work, p.rows, row, p.parts, part, p.top);
+                best = merged(best, 63 - lane < p.top ? list[63 - lane] : 0);
             }
+            lists[wave][lane] = best;
             __syncthreads();
-            write_best(p, row, list, p.top, t, 256, Row(a, p.scale));
+            if (wave == 0) {
+                for (int w = 1; w < 4; ++w) best = merged(best, lists[w][63 - lane]);
+                if (lane < p.top) write_one(p, row, lane, best, Row(a, p.scale));
+            }
             __syncthreads();
         }
     }
@@ -341,12 +418,12 @@ __global__ __launch_bounds__(256) void swr_logprob_back_kernel(LogProbParams p) 
 
 unsigned grid_of(int64_t blocks) { return (unsigned)std::max<int64_t>(1, std::min(blocks, kMostBlocks)); }
 
-// Waves of a row (or part).
-int waves_of(int64_t vocab) { return vocab <= 2048 ? 1 : vocab <= 16384 ? 4 : 16; }
+// Waves of a row (or part): its logits, 32 or 16 a lane at a time.
+int waves_of(int64_t vocab, int parts) { return vocab <= 2048 ? 1 : vocab <= 16384 || parts > 1 ? 4 : 16; }
 
 template <class E, bool TOP>
 hipError_t forward(const LogProbParams& p, hipStream_t st) {
-    const int waves = waves_of(p.vocab);
+    const int waves = waves_of(p.vocab, p.parts);
     const int64_t items = p.rows * p.parts;
     if (waves == 1)
         hipLaunchKernelGGL((swr_logprob_kernel<E, 1, TOP>), dim3(grid_of((items + 3) / 4)), dim3(256), 0, st, p);
@@ -370,10 +447,12 @@ hipError_t backward(const LogProbParams& p, hipStream_t st) {
 
 }  // namespace
 
-// Blocks that share a row: where few rows leave the GPU idle.
+// Blocks that share a row: where few rows leave the GPU idle, about as many as there are compute units, and
+// parts of 8192 logits and more.
 int logprob_parts(int64_t rows, int64_t vocab) {
-    if (waves_of(vocab) < 16) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(vocab / 65536, 256 / std::max<int64_t>(rows, 1)));
+    if (vocab <= 16384 || rows > 64) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(vocab / 8192, 64),
+                                                               256 / std::max<int64_t>(rows, 1)));
 }
 
 int64_t logprob_work_bytes(int64_t rows, int64_t vocab, int top) {
