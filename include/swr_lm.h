@@ -46,7 +46,7 @@ extern "C" {
  *
  * A token outside 0 .. vocab - 1 (padding) has a row of zeros and no part in the
  * gradient.  The gradient's rows of tokens that do not occur are zeros.  A token's
- * rows of dy are added in their order, in pieces of at most 64 rows whose sums are then
+ * rows of dy are added in their order, in pieces of at most 16 rows whose sums are then
  * added in order, in float32.
  * ------------------------------------------------------------------------ */
 

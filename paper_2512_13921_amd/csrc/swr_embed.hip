@@ -5,7 +5,7 @@
 // The forward moves its rows once.  The gradient sorts the positions by their tokens
 // (a radix sort that keeps the order of equal ones), so that a token's rows of dy are
 // added in order by one thread, without atomics, and its row of the gradient is written once.
-// The sorted positions are cut into windows of 32: a token's rows within one are
+// The sorted positions are cut into windows of 16: a token's rows within one are
 // summed in registers; sums that go on over a window's ends are kept as parts and
 // joined in order.  The gradient's rows are all set to zero beforehand, by further blocks of the sort's own
 // launches, which have little to do otherwise.
@@ -19,9 +19,10 @@
 namespace swr {
 namespace {
 
-constexpr int kSortThreads = 1024, kKeys = 4, kTileKeys = kSortThreads * kKeys, kDigits = 256;
+constexpr int kSortThreads = 1024, kKeys = 4, kTileKeys = kSortThreads * kKeys;
+constexpr int kBits = 9, kDigits = 1 << kBits;   // of a pass: two for 262143 tokens
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kWindow = 32;
+constexpr int kWindow = 16;
 constexpr int64_t kMostBlocks = 1 << 20;
 constexpr int64_t kSummed = 64;   // tiles whose counts the scatter adds up by itself
 
@@ -72,7 +73,7 @@ Sort layout(int64_t rows, int64_t vocab, void* work) {
     s.tiles = (rows + kTileKeys - 1) / kTileKeys;
     s.windows = (rows + kWindow - 1) / kWindow;
     while (((int64_t)1 << s.bits) <= vocab) ++s.bits;   // (vocab stands for a token that is none)
-    s.passes = (s.bits + 7) / 8;
+    s.passes = (s.bits + kBits - 1) / kBits;
     char* w = (char*)work;
     const auto take = [&](int64_t bytes) {
         char* at = w;
@@ -132,7 +133,7 @@ __device__ inline void count_digits(const uint32_t* digit, const bool* there, ui
     for (int k = 0; k < kKeys; ++k) {
         uint64_t same = __ballot(there[k]);
 #pragma unroll
-        for (int bit = 0; bit < 8; ++bit) {
+        for (int bit = 0; bit < kBits; ++bit) {
             const bool on = digit[k] >> bit & 1;
             const uint64_t with = __ballot(on);
             same &= on ? with : ~with;
@@ -160,20 +161,25 @@ __device__ inline void sum_waves(uint32_t (*count)[kDigits], uint32_t* total) {
     }
 }
 
-// In place of 256 values in LDS the sums of those before each; called by all threads of a block.
+// In place of a digit's values in LDS the sums of those before each; called by all threads of a block of kSortThreads.
 __device__ inline void sum_digits(uint32_t* v) {
-    const int t = threadIdx.x;
-    for (int reach = 1; reach < kDigits; reach *= 2) {
-        uint32_t add = 0;
-        if (t < kDigits && t >= reach) add = v[t - reach];
-        __syncthreads();
-        if (t < kDigits) v[t] += add;
-        __syncthreads();
+    __shared__ uint32_t totals[kDigits / 64];
+    const int t = threadIdx.x, lane = t % 64, wave = t / 64;
+    uint32_t own = 0, sum = 0;
+    if (t < kDigits) {
+        own = sum = v[t];
+#pragma unroll
+        for (int reach = 1; reach < 64; reach *= 2) {
+            const uint32_t add = __shfl_up(sum, reach);
+            if (lane >= reach) sum += add;
+        }
+        if (lane == 63) totals[wave] = sum;
     }
-    uint32_t before = 0;
-    if (t > 0 && t < kDigits) before = v[t - 1];
     __syncthreads();
-    if (t < kDigits) v[t] = before;
+    if (t < kDigits) {
+        for (int w = 0; w < wave; ++w) sum += totals[w];
+        v[t] = sum - own;
+    }
     __syncthreads();
 }
 
@@ -195,7 +201,7 @@ __global__ __launch_bounds__(kSortThreads) void swr_embed_sort_kernel(EmbedParam
         for (int i = threadIdx.x; i < kSortWaves * kDigits; i += kSortThreads) (&count[0][0])[i] = 0;
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kKeys; ++k) digit[k] = key[k] >> 8 * pass & 255;
+        for (int k = 0; k < kKeys; ++k) digit[k] = key[k] >> kBits * pass & (kDigits - 1);
         count_digits(digit, there, count, rank);
         __syncthreads();
         sum_waves(count, base);
@@ -242,7 +248,7 @@ __global__ __launch_bounds__(kSortThreads) void swr_embed_count_kernel(EmbedPara
 #pragma unroll
         for (int k = 0; k < kKeys; ++k) {
             const int64_t i = tile * kTileKeys + k * kSortThreads + threadIdx.x;
-            if (i < s.rows) atomicAdd(&count[(pass ? keys[i] : key_of(p, i)) >> 8 * pass & 255], 1u);
+            if (i < s.rows) atomicAdd(&count[(pass ? keys[i] : key_of(p, i)) >> kBits * pass & (kDigits - 1)], 1u);
         }
         __syncthreads();
         if (threadIdx.x < kDigits) s.counts[threadIdx.x * s.tiles + tile] = count[threadIdx.x];
@@ -252,18 +258,19 @@ __global__ __launch_bounds__(kSortThreads) void swr_embed_count_kernel(EmbedPara
 
 // In place of a digit's counts those of the tiles before (for many tiles), and the digit's total in the place
 // of its last tile's: a block a digit.
-__global__ __launch_bounds__(kDigits) void swr_embed_scan_kernel(Sort s) {
-    __shared__ uint32_t sums[kDigits];
+constexpr int kScanThreads = 256;
+__global__ __launch_bounds__(kScanThreads) void swr_embed_scan_kernel(Sort s) {
+    __shared__ uint32_t sums[kScanThreads];
     __shared__ uint32_t carry;
     uint32_t* counts = s.counts + (int64_t)blockIdx.x * s.tiles;
     if (threadIdx.x == 0) carry = 0;
-    for (int64_t first = 0; first < s.tiles; first += kDigits) {
+    for (int64_t first = 0; first < s.tiles; first += kScanThreads) {
         const int64_t i = first + threadIdx.x;
         const uint32_t own = i < s.tiles ? counts[i] : 0;
         __syncthreads();
         sums[threadIdx.x] = own;
         __syncthreads();
-        for (int reach = 1; reach < kDigits; reach *= 2) {
+        for (int reach = 1; reach < kScanThreads; reach *= 2) {
             const uint32_t add = (int)threadIdx.x >= reach ? sums[threadIdx.x - reach] : 0;
             __syncthreads();
             sums[threadIdx.x] += add;
@@ -271,7 +278,7 @@ __global__ __launch_bounds__(kDigits) void swr_embed_scan_kernel(Sort s) {
         }
         if (i < s.tiles) counts[i] = carry + sums[threadIdx.x];   // (of the tiles up to this one)
         __syncthreads();
-        if (threadIdx.x == 0) carry += sums[kDigits - 1];
+        if (threadIdx.x == 0) carry += sums[kScanThreads - 1];
     }
 }
 
@@ -316,7 +323,7 @@ __global__ __launch_bounds__(kSortThreads) void swr_embed_scatter_kernel(EmbedPa
                 key[k] = pass ? keys[i] : key_of(p, i);
                 place[k] = pass ? places[i] : (uint32_t)i;
             }
-            digit[k] = key[k] >> 8 * pass & 255;
+            digit[k] = key[k] >> kBits * pass & (kDigits - 1);
         }
         count_digits(digit, there, count, rank);
         __syncthreads();
@@ -403,15 +410,16 @@ __global__ __launch_bounds__(256) void swr_embed_window_kernel(EmbedParams p, So
 }
 
 // Sums of tokens that go on over windows' ends, each by the window that it begins in: that
-// window's part 1 and the part 0 of those that begin with the same token.
+// window's part 1 and the part 0 of those that begin with the same token.  A block's four waves take a quarter of
+// them each, one after the other, 64 vectors of 4 columns, and their sums are added in order.
+constexpr int kJoinVectors = 2;   // of a lane
 template <class OE>
-__global__ __launch_bounds__(256) void swr_embed_join_kernel(EmbedParams p, Sort s, int shift) {
+__global__ __launch_bounds__(256) void swr_embed_join_kernel(EmbedParams p, Sort s) {
     constexpr int NE = 4;
+    __shared__ float sums[3][kJoinVectors * NE][64];
     const uint32_t* keys = s.keys[s.passes % 2];
-    const int t = threadIdx.x & ((1 << shift) - 1);
-    const int64_t per_block = 256 >> shift;
-    for (int64_t w = blockIdx.x * per_block + (threadIdx.x >> shift); w + 1 < s.windows;
-         w += gridDim.x * per_block) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    for (int64_t w = blockIdx.x; w + 1 < s.windows; w += gridDim.x) {
         const int64_t first = w * kWindow;
         const uint32_t token = keys[first + kWindow - 1];
         // (it goes on, and begins in this window)
@@ -423,22 +431,42 @@ __global__ __launch_bounds__(256) void swr_embed_join_kernel(EmbedParams p, Sort
             if (keys[mid * kWindow] == token) low = mid;
             else high = mid;
         }
-        for (int64_t e = ((int64_t)blockIdx.y << shift) * NE + (int64_t)t * NE; e < p.width;
-             e += ((int64_t)gridDim.y << shift) * NE) {
-            const int left = (int)min(p.width - e, (int64_t)NE);
-            float sum[NE];
-            load<F32, NE>(s.parts + (2 * w + 1) * p.width, (int)e, (int)p.width, sum);
-#pragma unroll 8
-            for (int64_t k = w + 1; k <= low; ++k) {
-                float f[NE];
-                load<F32, NE>(s.parts + 2 * k * p.width, (int)e, (int)p.width, f);
+        // Parts 0 .. low - w: this window's part 1, then the others' part 0.
+        const int64_t parts = low - w + 1, each = (parts + 3) / 4, begin = min(wave * each, parts), end = min(begin + each, parts);
+        for (int64_t base = (int64_t)blockIdx.y * 64 * kJoinVectors * NE; base < p.width;
+             base += (int64_t)gridDim.y * 64 * kJoinVectors * NE) {
+            float sum[kJoinVectors][NE] = {};
+#pragma unroll 4
+            for (int64_t k = begin; k < end; ++k) {
+                const float* row = s.parts + (k == 0 ? 2 * w + 1 : 2 * (w + k)) * p.width;
 #pragma unroll
-                for (int c = 0; c < NE; ++c) sum[c] += f[c];
+                for (int v = 0; v < kJoinVectors; ++v) {
+                    const int64_t e = base + (v * 64 + lane) * NE;
+                    Slice<F32, NE> f;
+                    f.load(row, (int)min(e, p.width), (int)p.width);
+#pragma unroll
+                    for (int c = 0; c < NE; ++c) sum[v][c] += f[c];
+                }
             }
-            typename OE::store* out = (typename OE::store*)p.out + token * p.s_out + e;
+            if (wave > 0) {
 #pragma unroll
-            for (int c = 0; c < NE; ++c)
-                if (c < left) out[c] = OE::to(sum[c] * p.scale);
+                for (int i = 0; i < kJoinVectors * NE; ++i) sums[wave - 1][i][lane] = sum[i / NE][i % NE];
+            }
+            __syncthreads();
+            if (wave == 0) {
+#pragma unroll
+                for (int v = 0; v < kJoinVectors; ++v) {
+                    const int64_t e = base + (v * 64 + lane) * NE;
+                    typename OE::store* out = (typename OE::store*)p.out + token * p.s_out + e;
+#pragma unroll
+                    for (int c = 0; c < NE; ++c) {
+#pragma unroll
+                        for (int g = 0; g < 3; ++g) sum[v][c] += sums[g][v * NE + c][lane];
+                        if (e + c < p.width) out[c] = OE::to(sum[v][c] * p.scale);
+                    }
+                }
+            }
+            __syncthreads();
         }
     }
 }
@@ -467,7 +495,7 @@ hipError_t backward(const EmbedParams& p, void* work, hipStream_t st) {
                                Clear{blocks, 2 * pass, parts}, pass);
             if ((e = hipGetLastError()) != hipSuccess) return e;
             if (scanned) {
-                hipLaunchKernelGGL(swr_embed_scan_kernel, dim3(kDigits), dim3(kDigits), 0, st, s);
+                hipLaunchKernelGGL(swr_embed_scan_kernel, dim3(kDigits), dim3(kScanThreads), 0, st, s);
                 if ((e = hipGetLastError()) != hipSuccess) return e;
             }
             hipLaunchKernelGGL((swr_embed_scatter_kernel<OE>), dim3(grid), dim3(kSortThreads), 0, st, p, s,
@@ -479,17 +507,16 @@ hipError_t backward(const EmbedParams& p, void* work, hipStream_t st) {
         return (unsigned)std::max<int64_t>(1, std::min<int64_t>(1024, (p.width + ((int64_t)ne << shift) - 1) /
                                                                            ((int64_t)ne << shift)));
     };
-    int shift = row_shift((p.width + E::NE - 1) / E::NE);
-    int64_t per_block = 256 >> shift;
+    const int shift = row_shift((p.width + E::NE - 1) / E::NE);
+    const int64_t per_block = 256 >> shift;
     hipLaunchKernelGGL((swr_embed_window_kernel<E, OE>),
                        dim3(grid_of((s.windows + per_block - 1) / per_block), columns(E::NE, shift)), dim3(256), 0, st,
                        p, s, shift);
     if ((e = hipGetLastError()) != hipSuccess || s.windows == 1) return e;
-    shift = row_shift((p.width + 3) / 4);
-    per_block = 256 >> shift;
     hipLaunchKernelGGL((swr_embed_join_kernel<OE>),
-                       dim3(grid_of((s.windows + per_block - 1) / per_block), columns(4, shift)), dim3(256), 0, st, p,
-                       s, shift);
+                       dim3(grid_of(s.windows), (unsigned)std::min<int64_t>(1024, (p.width + 256 * kJoinVectors - 1) /
+                                                                                      (256 * kJoinVectors))),
+                       dim3(256), 0, st, p, s);
     return hipGetLastError();
 }
 
