@@ -275,32 +275,27 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void swr_logprob_ker
         const int64_t first = there ? tiles * part / p.parts : 0, last = there ? tiles * (part + 1) / p.parts : 0;
         Sums a{-__builtin_inff(), 0.0f, 0.0f};
         bool odd = false;   // a NaN, which a maximum passes over
-        for (int64_t tile = first; tile < last; ++tile) {
-            Slice<E, NE> v[kVectors];
-            const int64_t at = tile * kTile * size + (int64_t)t * NE;
+        struct Tile {
+            u32x4 v[kVectors];
+        } even, odd_tile;
+        const auto fetch = [&](Tile& tile, int64_t at) {   // a whole tile
+            const T* from = x + at * kTile * size + (int64_t)t * NE;
 #pragma unroll
-            for (int i = 0; i < kVectors; ++i) {
-                const int64_t e = at + (int64_t)i * size * NE;
-                if (e + NE <= p.vocab) v[i].v[0] = ((const Loose<T>*)(x + e))->v;
-                else {
-                    T tail[NE];
-#pragma unroll
-                    for (int c = 0; c < NE; ++c) tail[c] = e + c < p.vocab ? x[e + c] : E::to(-__builtin_inff());
-                    __builtin_memcpy(v[i].v, tail, sizeof v[i].v);
-                }
-            }
-            float top = v[0][0];
+            for (int i = 0; i < kVectors; ++i) tile.v[i] = ((const Loose<T>*)(from + (int64_t)i * size * NE))->v;
+        };
+        const auto take = [&](const Tile& tile) {
+            float top = E::get(tile.v[0], 0);
 #pragma unroll
             for (int i = 0; i < kVectors; ++i)
 #pragma unroll
-                for (int c = 0; c < NE; ++c) top = fmaxf(top, v[i][c]);
+                for (int c = 0; c < NE; ++c) top = fmaxf(top, E::get(tile.v[i], c));
             if (top > a.m) raise(a, top, k);
             const float m = origin(a.m);
 #pragma unroll
             for (int i = 0; i < kVectors; ++i)
 #pragma unroll
                 for (int c = 0; c < NE; ++c) {
-                    const float d = (v[i][c] - m) * k, e = __builtin_amdgcn_exp2f(d);
+                    const float d = (E::get(tile.v[i], c) - m) * k, e = __builtin_amdgcn_exp2f(d);
                     a.s += e;
                     a.u = fmaf(e, fmaxf(d, -160.0f), a.u);   // (2^-160 is 0 in float32)
                 }
@@ -308,8 +303,33 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void swr_logprob_ker
 #pragma unroll
                 for (int i = 0; i < kVectors; ++i)
 #pragma unroll
-                    for (int c = 0; c < NE; ++c) odd |= v[i][c] != v[i][c];
+                    for (int c = 0; c < NE; ++c) odd |= E::get(tile.v[i], c) != E::get(tile.v[i], c);
             }
+        };
+        // Whole tiles, the next one's loads ahead; then one that the row ends in.
+        const int64_t whole = min(last, p.vocab / ((int64_t)kTile * size));
+        if (first < whole) fetch(even, first);
+        for (int64_t tile = first; tile < whole; tile += 2) {
+            fetch(odd_tile, min(tile + 1, whole - 1));
+            take(even);
+            if (tile + 1 >= whole) break;
+            fetch(even, min(tile + 2, whole - 1));
+            take(odd_tile);
+        }
+        if (max(first, whole) < last) {
+            const int64_t at = max(first, whole) * kTile * size + (int64_t)t * NE;
+#pragma unroll
+            for (int i = 0; i < kVectors; ++i) {
+                const int64_t e = at + (int64_t)i * size * NE;
+                if (e + NE <= p.vocab) even.v[i] = ((const Loose<T>*)(x + e))->v;
+                else {
+                    T tail[NE];
+#pragma unroll
+                    for (int c = 0; c < NE; ++c) tail[c] = e + c < p.vocab ? x[e + c] : E::to(-__builtin_inff());
+                    __builtin_memcpy(&even.v[i], tail, sizeof even.v[i]);
+                }
+            }
+            take(even);
         }
         const int64_t begin = first * kTile * size, end = min(last * kTile * size, p.vocab);
         uint32_t largest = 0;
@@ -418,12 +438,15 @@ __global__ __launch_bounds__(256) void swr_logprob_back_kernel(LogProbParams p) 
 
 unsigned grid_of(int64_t blocks) { return (unsigned)std::max<int64_t>(1, std::min(blocks, kMostBlocks)); }
 
-// Waves of a row (or part): its logits, 32 or 16 a lane at a time.
-int waves_of(int64_t vocab, int parts) { return vocab <= 2048 ? 1 : vocab <= 16384 || parts > 1 ? 4 : 16; }
+// Waves of a row (or part), which take 32 (float32: 16) logits a lane at a time: 16 where there are too few rows (or
+// parts) for the GPU's compute units to have more than two each.
+int waves_of(int64_t rows, int64_t vocab, int parts) {
+    return vocab <= 2048 ? 1 : vocab <= 16384 || parts > 1 || rows > 512 ? 4 : 16;
+}
 
 template <class E, bool TOP>
 hipError_t forward(const LogProbParams& p, hipStream_t st) {
-    const int waves = waves_of(p.vocab, p.parts);
+    const int waves = waves_of(p.rows, p.vocab, p.parts);
     const int64_t items = p.rows * p.parts;
     if (waves == 1)
         hipLaunchKernelGGL((swr_logprob_kernel<E, 1, TOP>), dim3(grid_of((items + 3) / 4)), dim3(256), 0, st, p);
