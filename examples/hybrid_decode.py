@@ -88,7 +88,7 @@ class HybridDecoder:
         """Logits [batch, vocab] (float32) after one more token of each request."""
         slots, _, self.lengths, self.free_count = swr.swr_block_tables(
             self.lengths, self.one_more, self.table, self.free, self.free_count, self.page_size, self.batch)
-        h, y = self.embedding[tokens], None
+        h, y = swr.swr_embedding(tokens.contiguous(), self.embedding), None
         for i, kind in enumerate(self.layers):
             if y is None:
                 u, scale = swr.swr_rms_norm(h, self.norms[i], fp8=True)

@@ -534,6 +534,7 @@ def _channels(g):
 
 def _functions():
     torch = _torch()
+    once = torch.autograd.function.once_differentiable   # (a second derivative is refused)
 
     class _SWREmbeddingFunction(torch.autograd.Function):
         """Autograd wrapper of the embedding: y of (tokens, table, scale); the table's gradient
@@ -546,6 +547,7 @@ def _functions():
             return swr_embedding(tokens, table, scale)
 
         @staticmethod
+        @once
         def backward(ctx, dy):
             tokens, = ctx.saved_tensors
             return None, swr_embedding_backward(tokens, _even(dy), ctx.vocab, ctx.scale, ctx.dtype), None
@@ -560,6 +562,7 @@ def _functions():
             return swr_causal_conv(x, weight, bias, silu, lengths=lengths)[0]
 
         @staticmethod
+        @once
         def backward(ctx, dy):
             x, weight, bias, lengths = ctx.saved_tensors
             dx, dw, db = swr_causal_conv_backward(x, weight, _channels(dy), bias, ctx.silu, lengths)
@@ -579,6 +582,7 @@ def _functions():
             return y, h_last
 
         @staticmethod
+        @once
         def backward(ctx, dy, dh):
             x, dt, A, B, C, D, z, dt_bias, h0, lengths, carriers = ctx.saved_tensors
             if dy is None and dh is None:
@@ -601,6 +605,7 @@ def _functions():
             return logp, lse, entropy
 
         @staticmethod
+        @once
         def backward(ctx, dlogp, dlse, dentropy):
             logits, tokens, lse, entropy = ctx.saved_tensors
             if dlogp is None and dlse is None and dentropy is None:
