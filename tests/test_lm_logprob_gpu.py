@@ -128,6 +128,28 @@ def test_gradient(swr, dtype, rows, vocab):
         assert torch.equal(place, swr.swr_log_probs_backward(logits, tokens, lse, entropy, a, c, b, scale))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("vocab", [9, 5000, 40001])
+def test_gradient_far_out(swr, dtype, vocab):
+    """Rows whose lse holds nothing, or little, of what p goes by: all of a type's lowest value, or far from zero."""
+    low, up = torch.finfo(dtype).min, rand(30, (vocab,), F32, 2.0)
+    x = torch.stack([torch.full((vocab,), low), torch.full((vocab,), low), up * 8 - 70000, up + 5000, up - 255, up,
+                     torch.full((vocab,), -low)])
+    x[1, vocab // 2] = low / 2
+    x = x.to(dtype).cuda()
+    tokens = torch.tensor([3, 0, 1, vocab - 1, 2, -1, 7]).cuda()
+    a, b, c = (rand(i, (7,), F32).cuda() for i in (31, 32, 33))
+    _, lse, entropy = swr.swr_log_probs(x, tokens)
+    for dlogp, dlse, dentropy in ((a, None, None), (a, b, c), (None, None, None)):
+        want, size = ref.log_probs_backward(x, tokens, 1.0, dlogp, dlse, dentropy)
+        # As above, with an lse of at most 256 (farther out p goes by the distance from the row's largest logit).
+        bound = want.abs() * ROUND[dtype] + size * U * (2 * vocab + 8 * 256 + 500) * (1 + ROUND[dtype]) + TINY
+        d = swr.swr_log_probs_backward(x, tokens, lse, entropy, dlogp, dentropy, dlse)
+        ref.close(d, want, bound, "dlogits")
+        place = x.clone()
+        assert torch.equal(swr.swr_log_probs_backward(place, tokens, lse, entropy, dlogp, dentropy, dlse, dlogits=place), d)
+
+
 def test_layouts(swr):
     """Rows that are parts of wider ones, at odd addresses, and leading dimensions."""
     wide = rand(11, (3, 4, 3011), BF16).cuda()
