@@ -131,3 +131,22 @@ def test_refusals(swr):
             bad()
     with pytest.raises(swr.SwrError):
         swr.swr_embedding_backward(t, dy, 0)
+
+
+@pytest.mark.parametrize("n", [63, 64, 65, 1024, 4095, 4096, 4097])
+def test_orders_of_equal_tokens(swr, n):
+    """Sums whose order shows in their bits, repeated, of positions around a tile's and a block's."""
+    g = torch.Generator().manual_seed(n)
+    tokens = torch.randint(-1, 4, (n,), generator=g).cuda()
+    dy = (torch.randn(n, 3, generator=g) * 2.0 ** torch.randint(-20, 20, (n, 3), generator=g)).cuda()
+    first = swr.swr_embedding_backward(tokens, dy, 3)
+    for _ in range(3):
+        assert torch.equal(swr.swr_embedding_backward(tokens, dy, 3), first)
+    # Padding counts for nothing, NaN in its rows neither.
+    for v in range(3):
+        own = tokens == v
+        alone = swr.swr_embedding_backward(torch.where(own, tokens, -1), torch.where(own[:, None], dy, float("nan")), 3)
+        rows = ref.f64(dy[own])
+        ref.close(first[v], rows.sum(0), rows.abs().sum(0) * ref.U * n + ref.TINY, "sum")
+        ref.close(alone[v], rows.sum(0), rows.abs().sum(0) * ref.U * n + ref.TINY, "alone")
+        assert (alone[[i for i in range(3) if i != v]] == 0).all()
