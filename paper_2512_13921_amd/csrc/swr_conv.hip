@@ -104,7 +104,9 @@ __global__ __launch_bounds__(256) void swr_conv_kernel(ConvParams p, int shift, 
     const Taps<E, NE, K> taps(p, c);
     const int64_t per_block = 256 >> shift;
     for (int64_t u = blockIdx.y * per_block + (threadIdx.x >> shift); u < p.B * runs; u += gridDim.y * per_block) {
-        const int64_t b = u / runs, first = (u - b * runs) * kRun, end = min(first + kRun, p.T), live = tokens_of(p, b);
+        // (a division of 64 bits would cost a token alone as much as the rest)
+        const int64_t b = p.B * runs >> 32 ? u / runs : (int64_t)((uint32_t)u / (uint32_t)runs);
+        const int64_t first = (u - b * runs) * kRun, end = min(first + kRun, p.T), live = tokens_of(p, b);
         const T* x = (const T*)p.x + b * p.sx_b + c;
         T* y = (T*)p.y + b * p.sy_b + c;
         const T* state = p.state ? (const T*)p.state + b * (K - 1) * p.C + c : nullptr;
