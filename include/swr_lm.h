@@ -47,7 +47,7 @@ extern "C" {
  * A token outside 0 .. vocab - 1 (padding) has a row of zeros and no part in the
  * gradient.  The gradient's rows of tokens that do not occur are zeros.  A token's
  * rows of dy are added in their order, in pieces of at most 16 rows whose sums are then
- * added in order, in float32.
+ * added in four runs, the runs in order, in float32.
  * ------------------------------------------------------------------------ */
 
 typedef struct swr_embed {
@@ -141,7 +141,7 @@ typedef struct swr_scan {
     int64_t B, T, D, G;        /* G divides D                                             */
     int64_t sx_b, sx_t;        /* strides of x                                            */
     int64_t sdt_b, sdt_t;      /* ... of dt                                               */
-    int64_t sz_b, sz_t;        /* ... of z (not read without z)                           */
+    int64_t sz_b, sz_t;        /* ... of z (of no account without z)                    */
     int64_t sy_b, sy_t;        /* ... of y (the backward's dy)                            */
     int64_t sB_b, sB_t, sB_g;  /* ... of B                                                */
     int64_t sC_b, sC_t, sC_g;  /* ... of C                                                */
@@ -221,7 +221,8 @@ int64_t swr_log_probs_workspace_bytes(const swr_logprob_t* p);
 
 /* The logits' gradient, of the gradients of logp, lse and entropy (float32 [rows]; each may be NULL):
  *     dlogits[v] = scale (dlogp ([v = token] - p[v]) + dlse p[v] - dentropy p[v] (log p[v] + entropy))
- * lse and entropy are the forward's.  dlogits may be the logits themselves. */
+ * lse and entropy are the forward's (of rows with |lse| > 256, where float32 holds too little of it, the sum
+ * is taken anew).  dlogits may be the logits themselves. */
 int swr_log_probs_backward(const swr_logprob_t* p, const void* logits, const void* tokens, const float* lse,
                            const float* entropy, const float* dlogp, const float* dlse, const float* dentropy,
                            void* dlogits, void* stream);
