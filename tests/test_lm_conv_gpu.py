@@ -174,3 +174,25 @@ def test_autograd(swr):
     dx, dw = torch.autograd.grad(y, (x16, w16), dy)
     assert dw.dtype == BF16
     check_backward((dx, dw, None), x16.detach(), w16.detach(), None, True, dy)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_mixed_shapes(swr, seed):
+    """Shapes and options drawn at random; lengths, the state in place, NaN past the lengths."""
+    import random
+    rng = random.Random(seed)
+    B, T, C, K = rng.randint(1, 9), rng.choice((1, 2, rng.randint(1, 150))), rng.randint(1, 600), rng.randint(1, 8)
+    dtype, silu = rng.choice((BF16, F32)), rng.random() < 0.7
+    x, w, bias = make(60 + seed, B, T, C, K, dtype)
+    lengths = torch.tensor([rng.randint(0, T) for _ in range(B)], dtype=torch.int32).cuda()
+    for i, n in enumerate(lengths.tolist()):
+        x[i, n:] = float("nan")
+    state = rand(80, (B, K - 1, C), dtype).cuda()
+    before = state.clone()
+    y, last = swr.swr_causal_conv(x, w, bias, silu, state, lengths, state_out=state)
+    assert last is state
+    check_forward(y, x, w, bias, silu, before, lengths, state)
+    dy = rand(81, (B, T, C), dtype).cuda()
+    for i, n in enumerate(lengths.tolist()):
+        dy[i, n:] = float("inf")
+    check_backward(swr.swr_causal_conv_backward(x, w, dy, bias, silu, lengths), x, w, bias, silu, dy, lengths)

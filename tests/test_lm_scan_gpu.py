@@ -288,3 +288,48 @@ def test_far_rows(swr):
     got = swr.swr_selective_scan_backward(s["x"], s["dt"], s["A"], s["B"], s["C"], dy, carriers, s["D"], s["z"],
                                           s["dt_bias"])
     check_backward(s, r, got, dy)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T", [1, 2, 8, 9])
+@pytest.mark.parametrize("B,D,N,G", [(1, 5, 16, 5), (5, 130, 16, 2), (3, 7, 6, 1), (2, 9, 64, 9), (7, 6, 1, 3)])
+def test_few_tokens(swr, dtype, T, B, D, N, G):
+    """Odd numbers of batches, groups of one channel, lengths of all kinds, the state in place."""
+    lengths = [(T, 0, 1, T + 3, -1, T // 2, T - 1)[i] for i in range(B)]
+    s = make(40, B, T, D, N, G, dtype, h0=True, lengths=lengths)
+    for i, n in enumerate(lengths):
+        for k, t in enumerate((s["x"], s["dt"], s["B"], s["C"], s["z"])):
+            t[i, max(n, 0):] = (float("nan"), float("inf"))[(i + k) % 2]
+    r = definition(s)
+    y, carriers, h = swr.swr_selective_scan(**s, save_carriers=True, want_state=True)
+    check_forward(r, y, h, carriers)
+    state = s["h0"].clone()
+    again, none, last = swr.swr_selective_scan(**{**s, "h0": state}, h_last=state)
+    assert last is state and none is None and torch.equal(again, y) and torch.equal(state, h)
+    s["lengths"] = None
+    for k in ("x", "dt", "B", "C", "z"):
+        s[k] = torch.nan_to_num(s[k].contiguous(), 0.5, 0.5, -0.5)
+    bare = {**s, "h0": None, "z": None, "D": None, "dt_bias": None}
+    for given in (s, bare):
+        r = definition(given)
+        y, _, h = swr.swr_selective_scan(**given, want_state=True)
+        check_forward(r, y, h)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_mixed_shapes(swr, seed):
+    """Shapes and options drawn at random, forward and backward."""
+    import random
+    rng = random.Random(seed)
+    G, B, T, N = rng.choice((1, 1, 2, 5)), rng.randint(1, 5), rng.randint(1, 100), rng.randint(1, 64)
+    D, dtype = G * rng.randint(1, 40), rng.choice((BF16, F32))
+    lengths = [rng.randint(0, T) for _ in range(B)] if rng.random() < 0.6 else None
+    z, skip, bias, h0 = (rng.random() < 0.7 for _ in range(4))
+    s = make(50 + seed, B, T, D, N, G, dtype, z, skip, bias, h0, lengths)
+    r = definition(s)
+    y, carriers, h = swr.swr_selective_scan(**s, save_carriers=True, want_state=True)
+    check_forward(r, y, h, carriers)
+    dy, dh = rand(70, (B, T, D), dtype).cuda(), rand(71, (B, D, N), F32).cuda()
+    got = swr.swr_selective_scan_backward(s["x"], s["dt"], s["A"], s["B"], s["C"], dy, carriers, s["D"], s["z"],
+                                          s["dt_bias"], h0=s["h0"], dh_last=dh, lengths=s["lengths"], want_dh0=True)
+    check_backward(s, r, got, dy, dh)
