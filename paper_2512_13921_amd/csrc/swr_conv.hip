@@ -19,7 +19,6 @@ namespace swr {
 namespace {
 
 constexpr int kRun = 16;            // tokens of a thread, forward
-constexpr int kBackRun = 32;        // ... backward
 constexpr int kBackGroup = 4;       // tokens that the backward loads ahead
 constexpr int64_t kMostY = 32768;   // blocks of a launch in y, which take units in turn
 
@@ -171,7 +170,7 @@ __global__ __launch_bounds__(256) void swr_conv_kernel(ConvParams p, int shift, 
 // each of its waves; the waves' shares of dw and dbias are added in LDS, in order, and written as one row of `partial`.
 // (With eight bf16 channels a thread, of 272 registers, 5 x 4099 x 4096 took 274 us.)
 template <class E, int NE, int K, bool WHOLE, bool SILU>
-__global__ __launch_bounds__(256) void swr_conv_back_kernel(ConvParams p, int64_t runs) {
+__global__ __launch_bounds__(256) void swr_conv_back_kernel(ConvParams p, int run, int64_t runs) {
     typedef typename E::store T;
     typedef Row<E, NE> R;
     __shared__ float share[64 * NE * (K + 1)];
@@ -186,7 +185,7 @@ __global__ __launch_bounds__(256) void swr_conv_back_kernel(ConvParams p, int64_
         const Taps<E, NE, K> taps(p, c);
         for (int64_t u = blockIdx.y * 4 + wave; u < p.B * runs; u += gridDim.y * 4) {
             const int64_t b = u / runs;
-            const int first = (int)(u - b * runs) * kBackRun, end = (int)min((int64_t)first + kBackRun, p.T);
+            const int first = (int)(u - b * runs) * run, end = (int)min((int64_t)first + run, p.T);
             const int live = __builtin_amdgcn_readfirstlane((int)tokens_of(p, b));
             const T* x = (const T*)p.x + b * p.sx_b;
             const T* dy = (const T*)p.dy + b * p.sy_b;
@@ -207,8 +206,9 @@ __global__ __launch_bounds__(256) void swr_conv_back_kernel(ConvParams p, int64_
             struct Group {
                 R x[kBackGroup], dy[kBackGroup];
             } even, odd;
-            const int last = live - 1;
-            const auto fetch = [&](Group& v, int t) {   // (past the last token that one once more)
+            // (Past the last token that counts that one once more: it comes from a cache.)
+            const int last = min(live, end + K - 1) - 1;
+            const auto fetch = [&](Group& v, int t) {
 #pragma unroll
                 for (int i = 0; i < kBackGroup; ++i) {
                     const int at = min(t + i, last);
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(256) void swr_conv_back_kernel(ConvParams p, int64_
             const auto step = [&](const Group& v, int t) {
 #pragma unroll
                 for (int i = 0; i < kBackGroup; ++i) {
-                    const bool there = t + i < live, own = t + i < end;
+                    const bool there = t + i <= last, own = t + i < end;
 #pragma unroll
                     for (int k = 0; k + 1 < K; ++k) window[k] = window[k + 1];
                     window[K - 1] = v.x[i];
@@ -352,11 +352,18 @@ struct Forward {
 
 constexpr int kBackChannels = 4;   // of a thread
 
+// Tokens of a run, backward: long ones load fewer rows twice, short ones are more.  By the waves that runs of 32 make:
+// 1 x 2048 x 2048 (512 waves) takes 17.5 us in runs of 16, 23.1 of 32, 27.7 of 48; 8 x 1000 x 1000 (1024) 26.1, 23.7, 28.3;
+// 2 x 2048 x 4096 (2048) 37.0, 32.0, 38.4; 5 x 4099 x 4096 (10320) 126 of 32, 117 of 48, 129 of 64.
+int back_run(int64_t B, int64_t T, int64_t C) {
+    const int64_t waves = B * ((T + 31) / 32) * ((C + 64 * kBackChannels - 1) / (64 * kBackChannels));
+    return waves < 1024 ? 16 : waves < 8192 ? 32 : 48;
+}
 // Rows of partial sums: as many blocks as fill the GPU and no more than there are fours of runs.
 int64_t back_rows(int64_t B, int64_t T, int64_t C) {
-    const int64_t fours = (B * ((T + kBackRun - 1) / kBackRun) + 3) / 4, along = (C + 64 * kBackChannels - 1) /
-                                                                                  (64 * kBackChannels);
-    return std::max<int64_t>(1, std::min(fours, std::max<int64_t>(1, (1536 + along - 1) / along)));
+    const int run = back_run(B, T, C);
+    const int64_t fours = (B * ((T + run - 1) / run) + 3) / 4, along = (C + 64 * kBackChannels - 1) / (64 * kBackChannels);
+    return std::max<int64_t>(1, std::min(fours, std::max<int64_t>(1, (1024 + along - 1) / along)));
 }
 
 template <class E, int K>
@@ -364,13 +371,14 @@ struct Backward {
     static hipError_t run(const ConvParams& p, hipStream_t st) {
         constexpr int NE = kBackChannels;
         const int64_t along = (p.C + 64 * NE - 1) / (64 * NE), rows = back_rows(p.B, p.T, p.C);
-        const int64_t runs = (p.T + kBackRun - 1) / kBackRun;
+        const int run = back_run(p.B, p.T, p.C);
+        const int64_t runs = (p.T + run - 1) / run;
         const dim3 grid((unsigned)along, (unsigned)rows);
         const auto kernel = p.C % NE == 0 ? p.silu ? swr_conv_back_kernel<E, NE, K, true, true>
                                                    : swr_conv_back_kernel<E, NE, K, true, false>
                                           : p.silu ? swr_conv_back_kernel<E, NE, K, false, true>
                                                    : swr_conv_back_kernel<E, NE, K, false, false>;
-        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, p, runs);
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, p, run, runs);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         const int64_t blocks = std::min<int64_t>((p.C * (K + 1) + 63) / 64, 1 << 20);
