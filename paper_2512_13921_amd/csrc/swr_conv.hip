@@ -8,7 +8,8 @@
 // last K - 1 rows of x (and of g) in a window that moves along, so that every row is
 // loaded once but for the K - 1 before (and after) the run.
 //
-// What bounds it is the bytes.
+// What bounds it is the bytes: 5 x 4099 x 4096 bf16 with 4 taps take 72 us forward (336 MB, 4.7 TB/s) and 117
+// backward (504 MB and the rows around the runs).  A single token is latency, 5.6 us for 64 x 4096.
 #include <algorithm>
 #include <type_traits>
 

@@ -18,7 +18,8 @@
 //     dlogits = scale p (dlse - dlogp - dentropy (log p + entropy)) + scale dlogp at the token
 //
 // What bounds it is the bytes, with the vector unit close behind: a logit takes 10 operations, of
-// which the exponential counts four.
+// which the exponential counts two.  4095 rows of 65536 bf16 take 100 us forward (5.4 TB/s) and 194 for the gradient (5.5);
+// 8 rows with 20 alternatives 18, in launches and what each waits for.
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>

@@ -17,8 +17,9 @@
 // handed to the others; B and C of a tile are in LDS as floats, read by all.
 //
 // What bounds it is not the bytes but the vector unit: of each state a token takes an
-// exponential (a quarter of the rate), two products and two multiply-adds, 32
-// cycles of a SIMD for a wave's 64 states.
+// exponential (half the rate), two products and two multiply-adds, 24
+// cycles of a SIMD for a wave's 64 states.  16387 tokens of 4096 channels with 16 states take 490 us, which is 72 cycles
+// with the helpers' share; 2 x 2048 tokens 127 forward and 370 backward; one more token of 128 requests 17.5, at 4 TB/s.
 //
 // Where the channels alone do not fill the GPU, a sequence is cut into runs:
 // the first pass finds each run's states from zero and the sum of its steps (the
