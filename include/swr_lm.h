@@ -195,6 +195,8 @@ int64_t swr_selective_scan_backward_workspace_bytes(const swr_scan_t* p);
  * scored) has logp = 0 and no gradient by it.  Logits of -infinity have p = 0 and no
  * part in the entropy.  A row of nothing else has lse = -infinity, logp =
  * -infinity, entropy = 0 and no gradient; a row that holds NaN or +infinity has NaN there.
+ * Where scale times the largest logit leaves float32, lse is an infinity of its sign; logp, entropy and the
+ * gradient go by distances from the largest logit, and are as defined.
  * ------------------------------------------------------------------------ */
 
 #define SWR_TOP_MOST 64
@@ -221,7 +223,7 @@ int64_t swr_log_probs_workspace_bytes(const swr_logprob_t* p);
 
 /* The logits' gradient, of the gradients of logp, lse and entropy (float32 [rows]; each may be NULL):
  *     dlogits[v] = scale (dlogp ([v = token] - p[v]) + dlse p[v] - dentropy p[v] (log p[v] + entropy))
- * lse and entropy are the forward's (of rows with |lse| > 256, where float32 holds too little of it, the sum
+ * lse and entropy are the forward's (of rows with |lse| > 256, where float32 holds too little of it, or none, the sum
  * is taken anew).  dlogits may be the logits themselves. */
 int swr_log_probs_backward(const swr_logprob_t* p, const void* logits, const void* tokens, const float* lse,
                            const float* entropy, const float* dlogp, const float* dlse, const float* dentropy,

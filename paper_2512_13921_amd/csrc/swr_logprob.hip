@@ -398,7 +398,8 @@ __global__ __launch_bounds__(256) void swr_logprob_join_kernel(LogProbParams p) 
 // The gradient: blockIdx.y's rows in turn, a thread's vectors 256 apart.
 //
 // lse as a float32 is off by half its last place, and p by as much of itself: 2^-17 up to 256.  Of a row farther out (all
-// of a type's lowest value, say, where nothing of log V is left in lse) every block takes the largest logit and the sum anew;
+// of a type's lowest value, say, where nothing of log V is left in lse, or which is infinite as a float32 though no logit
+// is) every block takes the largest logit and the sum anew, and finds whether there is a logit above -infinity at all;
 // a call in place has one block a row, so that it has read the row before it writes to it.
 constexpr float kFar = 256.0f;
 // A row's largest logit and its sum by a block.  (A function of its own, for its registers: of 4095 rows of 65536 bf16 the
@@ -429,17 +430,19 @@ __global__ __launch_bounds__(256) void swr_logprob_back_kernel(LogProbParams p) 
         const float lse = p.lse_in[row], entropy = p.entropy_in[row];
         const float dlogp = scored && p.dlogp ? p.dlogp[row] : 0.0f, dlse = p.dlse ? p.dlse[row] : 0.0f;
         const float dentropy = p.dentropy ? p.dentropy[row] : 0.0f;
-        const bool empty = lse == -__builtin_inff();
+        bool empty = false;   // no logit above -infinity
         const float base = p.scale * (dlse - dlogp - dentropy * entropy), slope = -p.scale * dentropy;
         const float hit = p.scale * dlogp;
         const T* x = (const T*)p.logits + row * p.sl;
         T* out = (T*)p.dlogits + row * p.sd;
         // log p = (x - m) scale - off
         float m = 0.0f, off = lse;
-        if (fabsf(lse) > kFar && fabsf(lse) < __builtin_inff() && !(base == 0.0f && slope == 0.0f)) {
+        const bool still = base == 0.0f && slope == 0.0f;   // p does not count
+        if (fabsf(lse) > kFar && (!still || fabsf(lse) == __builtin_inff())) {   // (not of a row with NaN)
             const Sums a = anew<E>(x, p.vocab, p.scale * kLog2e, sums);
             m = a.m;
             off = kLn2 * log2f(a.s);
+            empty = a.s == 0.0f;
         }
         for (int64_t at = ((int64_t)blockIdx.x * 256 * kVectors + threadIdx.x) * NE; at < p.vocab;
              at += (int64_t)gridDim.x * 256 * kVectors * NE) {
