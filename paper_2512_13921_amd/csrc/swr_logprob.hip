@@ -430,19 +430,24 @@ __global__ __launch_bounds__(256) void swr_logprob_back_kernel(LogProbParams p) 
         const float lse = p.lse_in[row], entropy = p.entropy_in[row];
         const float dlogp = scored && p.dlogp ? p.dlogp[row] : 0.0f, dlse = p.dlse ? p.dlse[row] : 0.0f;
         const float dentropy = p.dentropy ? p.dentropy[row] : 0.0f;
-        bool empty = false;   // no logit above -infinity
-        const float base = p.scale * (dlse - dlogp - dentropy * entropy), slope = -p.scale * dentropy;
-        const float hit = p.scale * dlogp;
+        float base = p.scale * (dlse - dlogp - dentropy * entropy), slope = -p.scale * dentropy;
+        float hit = p.scale * dlogp;
         const T* x = (const T*)p.logits + row * p.sl;
         T* out = (T*)p.dlogits + row * p.sd;
         // log p = (x - m) scale - off
         float m = 0.0f, off = lse;
-        const bool still = base == 0.0f && slope == 0.0f;   // p does not count
-        if (fabsf(lse) > kFar && (!still || fabsf(lse) == __builtin_inff())) {   // (not of a row with NaN)
-            const Sums a = anew<E>(x, p.vocab, p.scale * kLog2e, sums);
-            m = a.m;
-            off = kLn2 * log2f(a.s);
-            empty = a.s == 0.0f;
+        // Far rows (none with NaN).  Where p does not count it is taken as 0: by their lse, as far from the logits as that may
+        // lie, it could be infinite, and its product with 0 no number.  (The token's own gradient needs to know of an empty row.)
+        if (fabsf(lse) > kFar) {
+            if (base == 0.0f && slope == 0.0f && (hit == 0.0f || fabsf(lse) < __builtin_inff())) {
+                off = __builtin_inff();
+            } else {
+                const Sums a = anew<E>(x, p.vocab, p.scale * kLog2e, sums);
+                const bool empty = a.s == 0.0f;   // (no logit above -infinity: p, and every gradient, is 0)
+                m = origin(a.m);
+                off = empty ? __builtin_inff() : kLn2 * log2f(a.s);
+                if (empty) base = slope = hit = 0.0f;
+            }
         }
         for (int64_t at = ((int64_t)blockIdx.x * 256 * kVectors + threadIdx.x) * NE; at < p.vocab;
              at += (int64_t)gridDim.x * 256 * kVectors * NE) {
@@ -461,8 +466,7 @@ __global__ __launch_bounds__(256) void swr_logprob_back_kernel(LogProbParams p) 
                     const float logs = fmaf(v[i][c] - m, p.scale, -off);
                     const float prob = __builtin_amdgcn_exp2f(logs * kLog2e);
                     f[c] = prob * fmaf(slope, fmaxf(logs, -110.0f), base);   // (exp(-110) is 0 in float32)
-                    if (empty) f[c] = 0.0f;
-                    else if (e + c == token && scored) f[c] += hit;
+                    if (e + c == token && scored) f[c] += hit;
                 }
                 if (e < p.vocab) store<E, NE>(out + e, (int)min(p.vocab - e, (int64_t)NE), f);
             }
