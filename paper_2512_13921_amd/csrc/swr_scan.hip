@@ -671,6 +671,13 @@ __global__ __launch_bounds__(192 * kWaves, R == 1 ? 6 : 3) void swr_scan_rows_ke
     }
 }
 
+// h 2^e, where 2^e alone may leave float32 (a run's decays grow it past that and enter 0, or take what is large
+// below it): the exponent's whole part goes into h's own.  |e| past 1024 makes 0 or infinity of any h, and 0 stays 0.
+__device__ inline float scaled(float h, float e) {
+    const float within = e > 1024.0f ? 1024.0f : e < -1024.0f ? -1024.0f : e, whole = __builtin_ceilf(within);
+    return __builtin_ldexpf(h * __builtin_amdgcn_exp2f(within - whole), (int)whole);   // (a factor of 1/2 to 1; NaN stays NaN)
+}
+
 // Chains the runs of a state: in place of a run's own states those that it starts from
 // (BACK: the gradient that reaches its last states).
 template <bool BACK>
@@ -689,7 +696,7 @@ __global__ __launch_bounds__(256) void swr_scan_chain_kernel(ScanParams p) {
             const int64_t c = BACK ? p.chunks - 1 - k : k;
             const float own = s[c * each], total = steps[c * p.D];
             s[c * each] = h;
-            h = fmaf(__builtin_amdgcn_exp2f(rate * total), h, own);
+            h = scaled(h, rate * total) + own;
         }
         s[BACK ? 0 : (p.chunks - 1) * each] = h;
     }
