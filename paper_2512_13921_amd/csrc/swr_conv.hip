@@ -242,8 +242,8 @@ __global__ __launch_bounds__(256) void swr_conv_back_kernel(ConvParams p, int ru
                         const float mine = own ? d : 0.0f;
 #pragma unroll
                         for (int k = 0; k < K; ++k) {
-                            // (past the last token the window holds it again, which may be infinite)
-                            const float xe = there ? window[k][e] : 0.0f;
+                            // (past the run's tokens, or the last, the window's may be infinite, 0 times which is NaN)
+                            const float xe = there && own ? window[k][e] : 0.0f;
                             sums[e][k] = fmaf(mine, xe, sums[e][k]);
                         }
                         sums[e][K] += mine;
