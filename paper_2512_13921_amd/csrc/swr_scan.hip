@@ -1082,7 +1082,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void swr_scan_back_kernel(ScanParam
                 float sum = 0.0f;
 #pragma unroll
                 for (int i = 0; i < kWaves; ++i) sum += lds_sum[i][tt][which][n];
-                if (tt < tokens && n < p.N) shares[tt * step + which * p.N + n] = sum;
+                // (past the batch's last token 0 times its state, which may be infinite)
+                if (tt < tokens && n < p.N) shares[tt * step + which * p.N + n] = t + tt < at.live ? sum : 0.0f;
             }
             buf ^= 1;
         }
@@ -1297,7 +1298,7 @@ __global__ __launch_bounds__(64 * kBackWaves) void swr_scan_back_rows_kernel(Sca
                 float sum = 0.0f;
 #pragma unroll
                 for (int i = 0; i < kBackWaves; ++i) sum += lds_sum[i][which][tt][m];
-                if (tt < tokens && m < p.N) shares[tt * step + which * p.N + m] = sum;
+                if (tt < tokens && m < p.N) shares[tt * step + which * p.N + m] = t + tt < at.live ? sum : 0.0f;   // (as above)
             }
             buf ^= 1;
         }

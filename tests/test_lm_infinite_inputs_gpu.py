@@ -43,3 +43,23 @@ def test_convolution(swr, dtype, K, at):
     same_kinds(got[0], want[0], "dx")
     same_kinds(got[1], want[1], "dw")
     assert torch.isinf(want[1][[3, 5]]).any() and not torch.isnan(want[1]).any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N", [3, 16, 20, 64])
+@pytest.mark.parametrize("T", [21, 200])
+def test_scan_past_the_lengths(swr, dtype, N, T):
+    """A state that is infinite at its batch's last token: outputs and gradients past it are zeros all the same."""
+    B, D, n = 3, 5, [T - 3, T - 11, T]
+    x, dt, z, dy = (rand(i, (B, T, D), dtype).cuda() for i in (1, 2, 3, 4))
+    b, c = (rand(i, (B, T, 1, N), dtype).cuda() for i in (5, 6))
+    A, dh = -torch.exp(rand(7, (D, N), F32)).cuda(), rand(8, (B, D, N), F32).cuda()
+    lengths = torch.tensor(n, dtype=torch.int32).cuda()
+    for i in range(B):
+        x[i, n[i] - 1, 1] = INF
+    y, carriers, h = swr.swr_selective_scan(x, dt, A, b, c, z=z, lengths=lengths, save_carriers=True, want_state=True)
+    assert not torch.isfinite(h[:, 1]).any() and torch.isfinite(h[:, [0, 2, 3, 4]]).all()
+    got = swr.swr_selective_scan_backward(x, dt, A, b, c, dy, carriers, z=z, dh_last=dh, lengths=lengths)
+    for i in range(B):
+        for t in (y, got[0], got[1], got[3], got[4], got[6]):
+            assert (t[i, n[i]:] == 0).all()
