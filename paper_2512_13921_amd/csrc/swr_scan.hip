@@ -706,8 +706,12 @@ __global__ __launch_bounds__(256) void swr_scan_chain_kernel(ScanParams p) {
 // and kTogether batches (divisions would cost as much as the rest), and no load is in a branch, so that all of them go
 // ahead together: what is not there is read from where something else is, and left out.  128 requests of 4096 channels
 // of 16 states take 18.2 us (21.7 with branches and divisions; one batch a thread 19.4, four 22.4).
+//
+// With LENGTHS a batch may have no token at all, and none of it is read then: its loads go to A (which has an element for
+// each channel, and for each state).  Without, the lengths' absence is looked at all the same: known to the compiler, it
+// orders the loads otherwise, and the 128 requests take 22.6 us; with the choice of A in both 19.2.
 constexpr int kTogether = 2;
-template <class E, int L, bool FULL>
+template <class E, int L, bool FULL, bool LENGTHS>
 __global__ __launch_bounds__(64 * kWaves) void swr_scan_step_kernel(ScanParams p) {
     typedef typename E::store T;
     constexpr int S = 4, M = kTogether;
@@ -762,12 +766,15 @@ __global__ __launch_bounds__(64 * kWaves) void swr_scan_step_kernel(ScanParams p
 #pragma unroll
                 for (int m = 0; m < M; ++m) {   // (past the batch's last token that one once more)
                     const int64_t tt = max(min(t, live[m] - 1), (int64_t)0);
-                    x[m] = ((const T*)p.in.x + b[m] * p.sx_b + tt * p.sx_t)[d];
-                    dt[m] = ((const T*)p.in.dt + b[m] * p.sdt_b + tt * p.sdt_t)[d];
-                    z[m] = (has_z ? (const T*)p.in.z + b[m] * p.sz_b + tt * p.sz_t
-                                  : (const T*)p.in.x + b[m] * p.sx_b + tt * p.sx_t)[d];
-                    bt[m] = shared((const T*)p.in.B + b[m] * p.sB_b + tt * p.sB_t + group * p.sB_g);
-                    ct[m] = shared((const T*)p.in.C + b[m] * p.sC_b + tt * p.sC_t + group * p.sC_g);
+                    const auto row = [&](const void* v, int64_t sb, int64_t s_t) {
+                        const T* at = (const T*)v + b[m] * sb + tt * s_t;
+                        return !LENGTHS || live[m] > 0 ? at : (const T*)p.in.A;
+                    };
+                    x[m] = row(p.in.x, p.sx_b, p.sx_t)[d];
+                    dt[m] = row(p.in.dt, p.sdt_b, p.sdt_t)[d];
+                    z[m] = (has_z ? row(p.in.z, p.sz_b, p.sz_t) : row(p.in.x, p.sx_b, p.sx_t))[d];
+                    bt[m] = shared(row((const T*)p.in.B + group * p.sB_g, p.sB_b, p.sB_t));
+                    ct[m] = shared(row((const T*)p.in.C + group * p.sC_g, p.sC_b, p.sC_t));
                 }
                 if (t == 0) {
 #pragma unroll
@@ -1407,7 +1414,8 @@ struct Step {
     hipError_t operator()() const {
         const dim3 grid((unsigned)p.tiles, (unsigned)std::min<int64_t>(p.G, 65535),
                         (unsigned)std::min<int64_t>((p.B + kTogether - 1) / kTogether, 65535));
-        hipLaunchKernelGGL((swr_scan_step_kernel<E, L, FULL>), grid, dim3(64 * kWaves), 0, st, p);
+        const auto kernel = p.in.lengths ? swr_scan_step_kernel<E, L, FULL, true> : swr_scan_step_kernel<E, L, FULL, false>;
+        hipLaunchKernelGGL(kernel, grid, dim3(64 * kWaves), 0, st, p);
         return hipGetLastError();
     }
 };
