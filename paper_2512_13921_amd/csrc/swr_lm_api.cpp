@@ -28,6 +28,42 @@ bool clashes(std::initializer_list<Span> out, std::initializer_list<Span> in) {
     }
     return false;
 }
+// A tensor of rows, [B, T] of them, as a call has it (p NULL: not there); sizes and strides in bytes.
+struct RowTensor {
+    const void* p;
+    int64_t sb, st, width;
+    Span span;
+};
+RowTensor rows_of(const void* p, int64_t sb, int64_t st, int64_t width, int es, int64_t bytes) {
+    // (unsigned: a dimension of one has any stride)
+    return {p, (int64_t)((uint64_t)sb * es), (int64_t)((uint64_t)st * es), width * es, span(p, bytes)};
+}
+// Whether a and b share a byte.  Parts of one larger tensor have its rows' strides, and lie between each other's
+// elements: theirs are compared row by row; others are taken to meet where their spans do.
+bool meet(int64_t B, int64_t T, const RowTensor& a, const RowTensor& b) {
+    if (!overlap(a.span, b.span)) return false;
+    if ((B > 1 && a.sb != b.sb) || (T > 1 && a.st != b.st)) return true;
+    const int64_t width = a.width > b.width ? a.width : b.width;
+    if (!apart({{B, a.sb}, {T, a.st}, {width, 1}})) return true;
+    // Some rows are (i sb + j st) apart, |i| < B and |j| < T: they meet where that is within their widths of the
+    // tensors' distance.  The lesser dimensions reach less far than a dimension's stride, so only its two multiples
+    // next to what is left count.
+    const Sorted s({{B, a.sb}, {T, a.st}});
+    const auto rows = [&](const auto& self, int dims, int64_t distance) -> bool {
+        if (dims == 0) return distance < a.width && -distance < b.width;
+        const Dim& d = s.d[dims - 1];
+        const int64_t below = distance / d.stride - (distance % d.stride < 0);
+        for (int64_t i = below; i <= below + 1; ++i)
+            if (i > -d.size && i < d.size && self(self, dims - 1, distance - i * d.stride)) return true;
+        return false;
+    };
+    return rows(rows, s.n, (int64_t)(b.span.lo - a.span.lo));
+}
+bool meets(int64_t B, int64_t T, const RowTensor& out, std::initializer_list<RowTensor> in) {
+    for (const RowTensor& t : in)
+        if (meet(B, T, out, t)) return true;
+    return false;
+}
 // Bytes that a tensor spans, or -1: its offsets are out of range.
 int64_t extent(std::initializer_list<Dim> dims, int es) {
     for (const Dim& d : dims)
@@ -249,7 +285,10 @@ int swr_causal_conv(const swr_conv_t* p, const void* x, const void* w, const voi
     if (!all_aligned({x, w, bias, state, y, state_out}, size_of(p->dtype)) || !aligned(lengths, 4)) return SWR_ERR_ALIGN;
     const Span so = span(keeps ? state_out : nullptr, s.state), ss = span(state, s.state);
     const Span sx = span(x, s.x), sw = span(w, s.w), sb = span(bias, s.bias), sl = span(lengths, s.lengths);
-    if (clashes({span(y, s.y), so}, {sx, sw, sb, sl}) || overlap(span(y, s.y), ss) || (state_out != state && overlap(so, ss)))
+    const int es = size_of(p->dtype);
+    if (clashes({span(y, s.y), so}, {sw, sb, sl}) || overlap(so, sx) || overlap(span(y, s.y), ss) ||
+        (state_out != state && overlap(so, ss)) ||
+        meet(p->B, p->T, rows_of(y, p->sy_b, p->sy_t, p->C, es, s.y), rows_of(x, p->sx_b, p->sx_t, p->C, es, s.x)))
         return SWR_ERR_ALIAS;
     swr::ConvParams q = conv_params(p, x, w, bias, lengths);
     q.state = s.state > 0 ? state : nullptr;
@@ -275,8 +314,13 @@ int swr_causal_conv_backward(const swr_conv_t* p, const void* x, const void* w, 
         !aligned(workspace, 16))
         return SWR_ERR_ALIGN;
     const int64_t work = swr::conv_work_bytes(p->B, p->T, p->C, p->taps);
+    const int es = size_of(p->dtype);
+    const Span sx = span(x, s.x), sy = span(dy, s.y);
     if (clashes({span(dx, s.dx), span(dw, p->C * p->taps * 4), span(dbias, p->C * 4), span(workspace, work)},
-                {span(x, s.x), span(w, s.w), span(bias, s.bias), span(dy, s.y), span(lengths, s.lengths)}))
+                {span(w, s.w), span(bias, s.bias), span(lengths, s.lengths)}) ||
+        clashes({span(dw, p->C * p->taps * 4), span(dbias, p->C * 4), span(workspace, work)}, {sx, sy}) ||
+        meets(p->B, p->T, rows_of(dx, p->sd_b, p->sd_t, p->C, es, s.dx),
+              {rows_of(x, p->sx_b, p->sx_t, p->C, es, s.x), rows_of(dy, p->sy_b, p->sy_t, p->C, es, s.y)}))
         return SWR_ERR_ALIAS;
     swr::ConvParams q = conv_params(p, x, w, bias, lengths);
     q.dy = dy; q.dx = dx; q.dw = dw; q.db = dbias; q.partial = (float*)workspace;
@@ -306,10 +350,16 @@ int swr_selective_scan(const swr_scan_t* p, const swr_scan_inputs_t* in, void* y
         return SWR_ERR_ALIGN;
     const Span sh = span(in->h0, s.state), so = span(h_last, s.state), sy = span(y, s.y), sc = span(carriers, s.carriers);
     const Span sw = span(workspace, work);
-    if (clashes({sy, sc, so, sw},
-                {span(in->x, s.x), span(in->dt, s.dt), span(in->A, s.A), span(in->B, s.B), span(in->C, s.C),
-                 span(in->bias, s.channel), span(in->skip, s.channel), span(in->z, s.z), span(in->lengths, s.lengths)}) ||
-        overlaps(sh, {sy, sc, sw}) || (h_last != in->h0 && overlap(sh, so)))
+    // (B's and C's rows of a token, G of N elements, count as one from the first to the last)
+    const int64_t wb = (p->G - 1) * p->sB_g + p->N, wc = (p->G - 1) * p->sC_g + p->N;
+    if (clashes({sy, sc, so, sw}, {span(in->A, s.A), span(in->bias, s.channel), span(in->skip, s.channel),
+                                   span(in->lengths, s.lengths)}) ||
+        clashes({sc, so, sw}, {span(in->x, s.x), span(in->dt, s.dt), span(in->B, s.B), span(in->C, s.C), span(in->z, s.z)}) ||
+        overlaps(sh, {sy, sc, sw}) || (h_last != in->h0 && overlap(sh, so)) ||
+        meets(p->B, p->T, rows_of(y, p->sy_b, p->sy_t, p->D, s.es, s.y),
+              {rows_of(in->x, p->sx_b, p->sx_t, p->D, s.es, s.x), rows_of(in->dt, p->sdt_b, p->sdt_t, p->D, s.es, s.dt),
+               rows_of(in->z, p->sz_b, p->sz_t, p->D, s.es, s.z), rows_of(in->B, p->sB_b, p->sB_t, wb, s.es, s.B),
+               rows_of(in->C, p->sC_b, p->sC_t, wc, s.es, s.C)}))
         return SWR_ERR_ALIAS;
     swr::ScanParams q = scan_params(p, in, plan);
     q.y = y; q.carriers = carriers; q.h_last = h_last;
@@ -408,7 +458,9 @@ int swr_log_probs_backward(const swr_logprob_t* p, const void* logits, const voi
         return SWR_ERR_ALIGN;
     const Span out = span(dlogits, gradient);
     const bool same = dlogits == logits && (p->sd == p->sl || p->rows == 1);
-    if ((!same && overlap(out, span(logits, bytes))) ||
+    const int es = size_of(p->dtype);
+    if ((!same && meet(1, p->rows, rows_of(dlogits, 0, p->sd, p->vocab, es, gradient),
+                       rows_of(logits, 0, p->sl, p->vocab, es, bytes))) ||
         overlaps(out, {span(tokens, p->rows * p->token_bytes), span(lse, p->rows * 4), span(entropy, p->rows * 4),
                        span(dlogp, p->rows * 4), span(dlse, p->rows * 4), span(dentropy, p->rows * 4)}))
         return SWR_ERR_ALIAS;
