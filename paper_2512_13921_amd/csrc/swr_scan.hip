@@ -712,11 +712,11 @@ __global__ __launch_bounds__(256) void swr_scan_chain_kernel(ScanParams p) {
 // orders the loads otherwise, and the 128 requests take 22.6 us; with the choice of A in both 19.2.
 constexpr int kTogether = 2;
 template <class E, int L, bool FULL, bool LENGTHS>
-__global__ __launch_bounds__(64 * kWaves) void swr_scan_step_kernel(ScanParams p) {
+__global__ __launch_bounds__(64 * kWaves) void swr_scan_step_kernel(ScanParams p, int64_t first_tile) {
     typedef typename E::store T;
     constexpr int S = 4, M = kTogether;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, n0 = lane % L * S;
-    int64_t tile = blockIdx.x;
+    int64_t tile = first_tile + blockIdx.x;
     if (p.tiles % 8 == 0) tile = tile % 8 * (p.tiles / 8) + tile / 8;   // (as in Place)
     const int64_t c = (tile * kWaves + wave) * (64 / L) + lane / L;
     if (c >= p.Dg) return;
@@ -1412,11 +1412,17 @@ struct Step {
     hipStream_t st;
     template <int L, int S, bool FULL>
     hipError_t operator()() const {
-        const dim3 grid((unsigned)p.tiles, (unsigned)std::min<int64_t>(p.G, 65535),
-                        (unsigned)std::min<int64_t>((p.B + kTogether - 1) / kTogether, 65535));
         const auto kernel = p.in.lengths ? swr_scan_step_kernel<E, L, FULL, true> : swr_scan_step_kernel<E, L, FULL, false>;
-        hipLaunchKernelGGL(kernel, grid, dim3(64 * kWaves), 0, st, p);
-        return hipGetLastError();
+        // (A launch has less than 2^32 threads along a dimension.)
+        constexpr int64_t kMostTiles = (int64_t)1 << 23;
+        for (int64_t first = 0; first < p.tiles; first += kMostTiles) {
+            const dim3 grid((unsigned)std::min(p.tiles - first, kMostTiles), (unsigned)std::min<int64_t>(p.G, 65535),
+                            (unsigned)std::min<int64_t>((p.B + kTogether - 1) / kTogether, 65535));
+            hipLaunchKernelGGL(kernel, grid, dim3(64 * kWaves), 0, st, p, first);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
     }
 };
 template <class E>
