@@ -766,15 +766,15 @@ __global__ __launch_bounds__(64 * kWaves) void swr_scan_step_kernel(ScanParams p
 #pragma unroll
                 for (int m = 0; m < M; ++m) {   // (past the batch's last token that one once more)
                     const int64_t tt = max(min(t, live[m] - 1), (int64_t)0);
-                    const auto row = [&](const void* v, int64_t sb, int64_t s_t) {
-                        const T* at = (const T*)v + b[m] * sb + tt * s_t;
+                    const auto row = [&](const void* v, int64_t sb, int64_t s_t, int64_t more = 0) {
+                        const T* at = (const T*)v + b[m] * sb + tt * s_t + more;
                         return !LENGTHS || live[m] > 0 ? at : (const T*)p.in.A;
                     };
                     x[m] = row(p.in.x, p.sx_b, p.sx_t)[d];
                     dt[m] = row(p.in.dt, p.sdt_b, p.sdt_t)[d];
                     z[m] = (has_z ? row(p.in.z, p.sz_b, p.sz_t) : row(p.in.x, p.sx_b, p.sx_t))[d];
-                    bt[m] = shared(row((const T*)p.in.B + group * p.sB_g, p.sB_b, p.sB_t));
-                    ct[m] = shared(row((const T*)p.in.C + group * p.sC_g, p.sC_b, p.sC_t));
+                    bt[m] = shared(row(p.in.B, p.sB_b, p.sB_t, group * p.sB_g));
+                    ct[m] = shared(row(p.in.C, p.sC_b, p.sC_t, group * p.sC_g));
                 }
                 if (t == 0) {
 #pragma unroll
