@@ -148,8 +148,8 @@ __device__ inline void count_digits(const uint32_t* digit, const bool* there, ui
     }
 }
 
-// In place of the waves' counts those of the waves before, and each digit's total.
-__device__ inline void sum_waves(uint32_t (*count)[kDigits], uint32_t* total) {
+// In place of the waves' counts those of the waves before.
+__device__ inline void sum_waves(uint32_t (*count)[kDigits]) {
     if (threadIdx.x < kDigits) {
         uint32_t sum = 0;
 #pragma unroll
@@ -158,7 +158,6 @@ __device__ inline void sum_waves(uint32_t (*count)[kDigits], uint32_t* total) {
             count[w][threadIdx.x] = sum;
             sum += c;
         }
-        total[threadIdx.x] = sum;
     }
 }
 
@@ -278,7 +277,7 @@ __global__ __launch_bounds__(kScanThreads) void swr_embed_scan_kernel(Sort s) {
 template <class OE>
 __global__ __launch_bounds__(kSortThreads) void swr_embed_scatter_kernel(EmbedParams p, Sort s, Clear c, int pass,
                                                                          bool scanned) {
-    __shared__ uint32_t count[kSortWaves][kDigits], base[kDigits], mine[kDigits], total[kDigits];
+    __shared__ uint32_t count[kSortWaves][kDigits], base[kDigits], mine[kDigits];
     if (clears<OE>(p, c)) return;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const uint32_t *keys = s.keys[pass % 2], *places = s.places[pass % 2];
@@ -319,7 +318,7 @@ __global__ __launch_bounds__(kSortThreads) void swr_embed_scatter_kernel(EmbedPa
         }
         count_digits(digit, there, count, rank);
         __syncthreads();
-        sum_waves(count, total);
+        sum_waves(count);
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kKeys; ++k) {
