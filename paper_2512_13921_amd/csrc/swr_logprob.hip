@@ -399,25 +399,44 @@ __global__ __launch_bounds__(256) void swr_logprob_join_kernel(LogProbParams p) 
 //
 // lse as a float32 is off by half its last place, and p by as much of itself: 2^-17 up to 256.  Of a row farther out (all
 // of a type's lowest value, say, where nothing of log V is left in lse, or which is infinite as a float32 though no logit
-// is) every block takes the largest logit and the sum anew, and finds whether there is a logit above -infinity at all;
-// a call in place has one block a row, so that it has read the row before it writes to it.
+// is) one block takes the largest logit and the sum anew, finds whether there is a logit above -infinity at all, and writes the
+// row's gradient: it has read the row before it writes to it, as a call in place needs.  4095 far rows of 65536 bf16 take 440 us,
+// ordinary ones 190 (4757 with all of a row's blocks at it, each for itself).
 constexpr float kFar = 256.0f;
-// A row's largest logit and its sum by a block.  (A function of its own, for its registers: of 4095 rows of 65536 bf16 the
-// gradient takes 194 us, without such rows 185, with these lines in the kernel 211.)
+// A row's largest logit and its sum by a block.  (A function of its own, and one vector of a thread at a time, for the
+// registers: of 4095 rows of 65536 bf16 the kernel takes 190 us, 205 with four vectors, of 91 registers for 80; with these
+// lines in the kernel it took 211.)
 template <class E>
 __device__ __attribute__((noinline)) Sums anew(const typename E::store* x, int64_t vocab, float k, Sums* sums) {
+    constexpr int NE = E::NE;
     Sums a{-__builtin_inff(), 0.0f, 0.0f};
 #pragma unroll 1
-    for (int64_t e = threadIdx.x; e < vocab; e += 256) {
-        const float v = E::one(x[e]);
-        if (v > a.m) raise(a, v, k);
-        a.s += __builtin_amdgcn_exp2f((v - origin(a.m)) * k);
+    for (int64_t e = (int64_t)threadIdx.x * NE; e < vocab; e += 256 * NE) {
+        u32x4 v;
+        if (e + NE <= vocab) v = ((const Loose<typename E::store>*)(x + e))->v;
+        else {
+            typename E::store tail[NE];
+#pragma unroll
+            for (int c = 0; c < NE; ++c) tail[c] = e + c < vocab ? x[e + c] : E::to(-__builtin_inff());
+            __builtin_memcpy(&v, tail, sizeof v);
+        }
+        float top = E::get(v, 0);
+#pragma unroll
+        for (int c = 1; c < NE; ++c) top = fmaxf(top, E::get(v, c));
+        if (top > a.m) raise(a, top, k);
+        const float m = origin(a.m);
+#pragma unroll
+        for (int c = 0; c < NE; ++c) a.s += __builtin_amdgcn_exp2f((E::get(v, c) - m) * k);
     }
     a = wave_join(a, k);
     __syncthreads();   // (the last row's have been read)
     if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = a;
     __syncthreads();
     return join(join(sums[0], sums[1], k), join(sums[2], sums[3], k), k);
+}
+// A block's own value, in a scalar register.
+__device__ inline float uniform(float v) {
+    return as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__builtin_bit_cast(uint32_t, v)));
 }
 template <class E>
 __global__ __launch_bounds__(256) void swr_logprob_back_kernel(LogProbParams p) {
@@ -430,27 +449,32 @@ __global__ __launch_bounds__(256) void swr_logprob_back_kernel(LogProbParams p) 
         const float lse = p.lse_in[row], entropy = p.entropy_in[row];
         const float dlogp = scored && p.dlogp ? p.dlogp[row] : 0.0f, dlse = p.dlse ? p.dlse[row] : 0.0f;
         const float dentropy = p.dentropy ? p.dentropy[row] : 0.0f;
-        float base = p.scale * (dlse - dlogp - dentropy * entropy), slope = -p.scale * dentropy;
-        float hit = p.scale * dlogp;
+        float base = uniform(p.scale * (dlse - dlogp - dentropy * entropy)), slope = uniform(-p.scale * dentropy);
+        float hit = uniform(p.scale * dlogp);
         const T* x = (const T*)p.logits + row * p.sl;
         T* out = (T*)p.dlogits + row * p.sd;
         // log p = (x - m) scale - off
         float m = 0.0f, off = lse;
+        int64_t block = blockIdx.x, blocks = gridDim.x;   // of the row
         // Far rows (none with NaN).  Where p does not count it is taken as 0: by their lse, as far from the logits as that may
         // lie, it could be infinite, and its product with 0 no number.  (The token's own gradient needs to know of an empty row.)
         if (fabsf(lse) > kFar) {
             if (base == 0.0f && slope == 0.0f && (hit == 0.0f || fabsf(lse) < __builtin_inff())) {
                 off = __builtin_inff();
             } else {
+                // (rows' blocks go to the 8 dies in turn, and so do one of each)
+                if (block != row % blocks) continue;
+                block = 0;
+                blocks = 1;
                 const Sums a = anew<E>(x, p.vocab, p.scale * kLog2e, sums);
-                const bool empty = a.s == 0.0f;   // (no logit above -infinity: p, and every gradient, is 0)
-                m = origin(a.m);
-                off = empty ? __builtin_inff() : kLn2 * log2f(a.s);
+                const bool empty = uniform(a.s) == 0.0f;   // (no logit above -infinity: p, and every gradient, is 0)
+                m = uniform(origin(a.m));
+                off = uniform(empty ? __builtin_inff() : kLn2 * log2f(a.s));
                 if (empty) base = slope = hit = 0.0f;
             }
         }
-        for (int64_t at = ((int64_t)blockIdx.x * 256 * kVectors + threadIdx.x) * NE; at < p.vocab;
-             at += (int64_t)gridDim.x * 256 * kVectors * NE) {
+        for (int64_t at = (block * 256 * kVectors + threadIdx.x) * NE; at < p.vocab;
+             at += blocks * 256 * kVectors * NE) {
             Slice<E, NE> v[kVectors];
 #pragma unroll
             for (int i = 0; i < kVectors; ++i) {
@@ -500,8 +524,7 @@ hipError_t forward(const LogProbParams& p, hipStream_t st) {
 
 template <class E>
 hipError_t backward(const LogProbParams& p, hipStream_t st) {
-    const int64_t blocks = p.dlogits == p.logits ? 1 : std::min<int64_t>((p.vocab + 512 * E::NE - 1) / (512 * E::NE),
-                                                                         1 << 15);
+    const int64_t blocks = std::min<int64_t>((p.vocab + 512 * E::NE - 1) / (512 * E::NE), 1 << 15);
     hipLaunchKernelGGL((swr_logprob_back_kernel<E>), dim3((unsigned)blocks, (unsigned)std::min<int64_t>(p.rows, 32768)),
                        dim3(256), 0, st, p);
     return hipGetLastError();
