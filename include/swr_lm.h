@@ -22,7 +22,9 @@
  * the kernels: none of them can make one read or write out of bounds.
  *
  * Strides are in elements and may not be negative; elements of the innermost
- * dimension are contiguous.  Pointers are aligned to their elements (rows that
+ * dimension are contiguous.  Outputs may not share an element with an input or another output unless said otherwise;
+ * those with strides may lie between the elements of inputs of the same strides (parts of one tensor's rows), the others'
+ * address ranges are apart.  Pointers are aligned to their elements (rows that
  * are 16-byte aligned are read fastest), workspaces to 16 bytes.  Sums and
  * states are in float32; each output is rounded once, as it is stored.  Sums have a fixed
  * order: repeated calls give the same bits.
@@ -125,6 +127,10 @@ int64_t swr_causal_conv_workspace_bytes(const swr_conv_t* p);
  * h before the first token is h0, or zero.  With `lengths`, batch b has lengths[b] tokens (taken
  * within 0 and T): y, and the gradients, are zero past them, the inputs are not read
  * there, and the final state is the last token's.
+ *
+ * A token's own decay exp(s A) is a float32, and past its range infinite (times a state of 0 it is NaN); the
+ * product of many tokens' may be past it, only the states count.  Gradients of a channel whose state is infinite or
+ * NaN are infinite or NaN where the state counts, which of the two is not said.
  *
  * Carriers are the states before every SWR_SCAN_BLOCK tokens, float32
  * [B, ceil(T / SWR_SCAN_BLOCK), D, N]: the forward saves them for the backward.

@@ -18,7 +18,7 @@
 //     dlogits = scale p (dlse - dlogp - dentropy (log p + entropy)) + scale dlogp at the token
 //
 // What bounds it is the bytes, with the vector unit close behind: a logit takes 10 operations, of
-// which the exponential counts two.  4095 rows of 65536 bf16 take 100 us forward (5.4 TB/s) and 194 for the gradient (5.5);
+// which the exponential counts two.  4095 rows of 65536 bf16 take 100 us forward (5.4 TB/s) and 195 for the gradient (5.5);
 // 8 rows with 20 alternatives 18, in launches and what each waits for.
 #include <algorithm>
 #include <cfloat>
@@ -401,10 +401,10 @@ __global__ __launch_bounds__(256) void swr_logprob_join_kernel(LogProbParams p) 
 // of a type's lowest value, say, where nothing of log V is left in lse, or which is infinite as a float32 though no logit
 // is) one block takes the largest logit and the sum anew, finds whether there is a logit above -infinity at all, and writes the
 // row's gradient: it has read the row before it writes to it, as a call in place needs.  4095 far rows of 65536 bf16 take 440 us,
-// ordinary ones 190 (4757 with all of a row's blocks at it, each for itself).
+// ordinary ones 195 (4757 with all of a row's blocks at it, each for itself).
 constexpr float kFar = 256.0f;
 // A row's largest logit and its sum by a block.  (A function of its own, and one vector of a thread at a time, for the
-// registers: of 4095 rows of 65536 bf16 the kernel takes 190 us, 205 with four vectors, of 91 registers for 80; with these
+// registers: of 4095 rows of 65536 bf16 the kernel takes 195 us, 210 with four vectors, of 91 registers for 80; with these
 // lines in the kernel it took 211.)
 template <class E>
 __device__ __attribute__((noinline)) Sums anew(const typename E::store* x, int64_t vocab, float k, Sums* sums) {

@@ -19,7 +19,7 @@
 // What bounds it is not the bytes but the vector unit: of each state a token takes an
 // exponential (half the rate), two products and two multiply-adds, 24
 // cycles of a SIMD for a wave's 64 states.  16387 tokens of 4096 channels with 16 states take 490 us, which is 72 cycles
-// with the helpers' share; 2 x 2048 tokens 127 forward and 370 backward; one more token of 128 requests 17.5, at 4 TB/s.
+// with the helpers' share; 2 x 2048 tokens 127 forward and 370 backward; one more token of 128 requests 17.4, at 4.1 TB/s.
 //
 // Where the channels alone do not fill the GPU, a sequence is cut into runs:
 // the first pass finds each run's states from zero and the sum of its steps (the
@@ -705,7 +705,7 @@ __global__ __launch_bounds__(256) void swr_scan_chain_kernel(ScanParams p) {
 // A few tokens: no tiles, nothing shared, a token after the other; the states move once.  Blocks are channels, groups
 // and kTogether batches (divisions would cost as much as the rest), and no load is in a branch, so that all of them go
 // ahead together: what is not there is read from where something else is, and left out.  128 requests of 4096 channels
-// of 16 states take 18.2 us (21.7 with branches and divisions; one batch a thread 19.4, four 22.4).
+// of 16 states take 17.4 us (21.7 with branches and divisions; one batch a thread 19.4, four 22.4).
 //
 // With LENGTHS a batch may have no token at all, and none of it is read then: its loads go to A (which has an element for
 // each channel, and for each state).  Without, the lengths' absence is looked at all the same: known to the compiler, it
@@ -1522,7 +1522,9 @@ ScanPlan plan_scan(const swr_scan_t& p, bool backward) {
     for (const int64_t s : {p.sx_t, p.sdt_t, p.sz_t, p.sy_t, p.sB_t, p.sC_t}) near = near && s <= 1 << 22;
     ScanPlan plan = make(p.N > 8 && near ? 1 : 4);
     const int64_t waves = plan.states == 1 && backward ? kBackWaves : kWaves;
-    // Runs of at least 64 tokens, as many as give every SIMD a wave.
+    // Runs of at least 64 tokens, as many as give every SIMD a wave.  8192 tokens of 16 states cut and whole: of 1024
+    // channels 113 and 240 us forward, 487 and 1460 backward; of 2048 208 and 241, 957 and 1443; of 2560 to 3584, in two runs,
+    // 300 and 242, 1032 and 1530 (a forward there would be faster whole); of 4 states and 2048 channels 171 and 3017, 272 and 5322.
     const int64_t one = std::max<int64_t>(1, plan.blocks(p.B, p.G) * waves);   // (a batch of none has none)
     const int64_t most = std::max<int64_t>(1, p.T / 64);
     const int64_t chunks = std::min(most, (kWant + one - 1) / one);
