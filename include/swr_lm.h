@@ -22,12 +22,15 @@
  * the kernels: none of them can make one read or write out of bounds.
  *
  * Strides are in elements and may not be negative; elements of the innermost
- * dimension are contiguous.  Outputs may not share an element with an input or another output unless said otherwise;
- * those with strides may lie between the elements of inputs of the same strides (parts of one tensor's rows), the others'
- * address ranges are apart.  Pointers are aligned to their elements (rows that
+ * dimension are contiguous.  Pointers are aligned to their elements (rows that
  * are 16-byte aligned are read fastest), workspaces to 16 bytes.  Sums and
  * states are in float32; each output is rounded once, as it is stored.  Sums have a fixed
  * order: repeated calls give the same bits.
+ *
+ * Overlaps.  Outputs share no element with an input or another output unless said
+ * otherwise.  The convolution's y and dx, the scan's y and dlogits may lie between
+ * the elements of inputs of the same strides, as parts of one tensor's rows; the address
+ * ranges of all other outputs, and beside inputs of other strides, have to be apart.
  */
 #ifndef SWR_LM_H
 #define SWR_LM_H
